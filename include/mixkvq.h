@@ -42,7 +42,8 @@ extern "C" {
 #define MIXKVQ_EHIP      (-3)  /* a HIP call failed; mixkvq_strerror gives the HIP message */
 #define MIXKVQ_ENOMEM    (-4)  /* host allocation of the handle failed */
 #define MIXKVQ_EEMPTY    (-5)  /* decode attention on a cache that holds no token */
-#define MIXKVQ_ESCRATCH  (-7)  /* mixkvq_decode_attention_noalloc: the launch needs more than the built-in scratch buffer */
+#define MIXKVQ_ESCRATCH  (-7)  /* the launch needs more scratch than the built-in buffer (mixkvq_decode_attention_noalloc) or
+                                * the caller's workspace (mixkvq_chunk_attention, mixkvq_verify_draft) has */
 #define MIXKVQ_ERAGGED   (-6)  /* mixkvq_cache_state on a batch whose sequences differ: use mixkvq_cache_state_seq */
 
 typedef struct mixkvq_cache mixkvq_cache; /* opaque HOST handle: counts + the caller's device pointers */
@@ -237,6 +238,51 @@ int mixkvq_decode_attention_noalloc(mixkvq_cache* c, const void* q, void* out, f
  * fails after those (EHIP), the packed blocks stay packed and the new token is not appended. */
 int mixkvq_decode_step(mixkvq_cache* c, const void* k_new, const void* v_new, const int64_t kv_strides[3],
                        const void* q, void* out, float* lse, float scale, int32_t accumulate_q, void* stream);
+
+/* Several new tokens of every sequence at once, without appending them: a piece of a prompt behind its cached prefix, or the
+ * drafted tokens of a speculative step (Eq. 1 over the keys/values dequantized by Eq. 3, and over the chunk itself).  New
+ * token i of sequence b attends over everything the cache holds of the sequence and over new tokens 0 .. i.  The cache is
+ * not changed, so what is not wanted needs no taking back: append the tokens that stay afterwards (mixkvq_prefill,
+ * mixkvq_quantize_append, or mixkvq_quantize_append_seq with the accepted ones of one sequence).
+ *   q    DEVICE fp16 [B][Hq][n_new][D] after rotary embedding, element strides q_strides = {batch, head, token}.
+ *   k_new, v_new  DEVICE fp16 [B][Hkv][n_new][D], strides kv_strides likewise; they enter as the cache would keep them.
+ *   n_seq  HOST int32 [B] or NULL: new tokens of each sequence, 0 .. n_new (NULL: n_new for all).  Rows of q, k_new and v_new
+ *        behind them are not read, rows of out and lse behind them are left as they are.
+ *   out  DEVICE fp16 [B][Hq][n_new][D], strides out_strides;  lse DEVICE fp32 [B][Hq][n_new] contiguous, or NULL.
+ *   Channel stride 1; q, k_new, v_new and out start on 16 bytes and their strides are multiples of 8.  n_new <= 2^20.
+ *   scale <= 0 means 1/sqrt(D).  accumulate_q != 0 also adds |q| of all the new tokens to the accumulator (Appendix D.2).
+ *   workspace  DEVICE, on 16 bytes, at least mixkvq_chunk_workspace(c, n_new, n_seq) bytes for the cache's state at the call (NULL if
+ *        that is 0), else ESCRATCH.  It needs no clearing and holds nothing between calls; calls that may overlap
+ *        (two streams, two captured graphs) need one each.
+ * Any cache state, configuration and storage layout; the sequences may differ in length whatever B is.  Precision:
+ * dequantized keys and values and the weights of the softmax are rounded to binary16 (saturating) before the products, sums are
+ * binary32; the bound of mixkvq_decode_attention holds. */
+int64_t mixkvq_chunk_workspace(const mixkvq_cache* c, int32_t n_new, const int32_t* n_seq);   /* bytes, or a negative code */
+int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strides[3], const void* k_new, const void* v_new,
+                           const int64_t kv_strides[3], int32_t n_new, const int32_t* n_seq, void* out,
+                           const int64_t out_strides[3], float* lse, float scale, int32_t accumulate_q, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/* Drafted tokens against the target's probabilities, with given random numbers (the verdict of a speculative step, whose
+ * target pass is mixkvq_chunk_attention's).  Draft i of a sequence stays if all before it do and
+ *   u_accept[i] * p_draft[i][draft[i]] < p_target[i][draft[i]].
+ * With r drafts that stay, the next token is the smallest t with sum_{s <= t} w_s > u_next * sum_s w_s, the weights being
+ * max(p_target[r] - p_draft[r], 0) if draft r was rejected (p_target[r] where all of these are 0), and p_target[r] if all
+ * drafts stayed.  Products and sums are binary64.  If no sum is that large (u_next = 1) it is the last token with a weight
+ * above 0, and token 0 if there is none.
+ *   p_target  DEVICE fp32 [B][n_draft + 1][V], element strides {sequence, position}, vocabulary stride 1.
+ *   p_draft   DEVICE fp32 [B][n_draft][V] likewise, or NULL: all of a draft's probability is on its token (looked-up drafts).
+ *   draft     DEVICE int32 [B][n_draft] contiguous.  A token outside 0 .. V - 1 is rejected.
+ *   n_seq     DEVICE int32 [B] or NULL: drafts of each sequence (cut to 0 .. n_draft; NULL: n_draft for all).
+ *   u_accept  DEVICE fp32 [B][n_draft], u_next DEVICE fp32 [B]: uniform in [0, 1).
+ *   n_accepted DEVICE int32 [B];  tokens DEVICE int32 [B][n_draft + 1]: the drafts that stay, the next token, then -1.
+ *   workspace DEVICE, on 16 bytes, mixkvq_verify_workspace(B, V) bytes (else ESCRATCH); one for every call that may overlap.
+ * n_draft <= 64 (0: draws from p_target); draft and u_accept may be NULL if it is 0.  Needs no cache. */
+int64_t mixkvq_verify_workspace(int32_t B, int32_t V);   /* bytes, or a negative code */
+int mixkvq_verify_draft(int32_t B, int32_t n_draft, int32_t V, const float* p_target, const int64_t p_target_strides[2],
+                        const float* p_draft, const int64_t p_draft_strides[2], const int32_t* draft, const int32_t* n_seq,
+                        const float* u_accept, const float* u_next, int32_t* n_accepted, int32_t* tokens, void* workspace,
+                        int64_t workspace_bytes, void* stream);
 
 /* Profiling aid.  With a pair of hipEvent_t handles (HOST, created by the caller with timing enabled), every
  * following mixkvq_decode_attention / mixkvq_decode_step on this cache makes start_event and stop_event take the start

@@ -21,6 +21,7 @@ EXPORTS = ("mixkvq_block_layout", "mixkvq_cache_sizes", "mixkvq_cache_create", "
            "mixkvq_cache_set_block_table", "mixkvq_cache_set_state", "mixkvq_cache_set_state_seq", "mixkvq_cache_reset", "mixkvq_cache_reset_seq", "mixkvq_cache_state", "mixkvq_cache_state_seq",
            "mixkvq_select_channels", "mixkvq_select_channels_seq", "mixkvq_quantize_append", "mixkvq_quantize_append_seq", "mixkvq_prefill",
            "mixkvq_decode_attention", "mixkvq_decode_attention_noalloc", "mixkvq_decode_step", "mixkvq_set_timing_events", "mixkvq_decode_path",
+           "mixkvq_chunk_workspace", "mixkvq_chunk_attention", "mixkvq_verify_workspace", "mixkvq_verify_draft",
            "mixkvq_strerror")
 
 
@@ -86,11 +87,16 @@ def load_library() -> C.CDLL:
     lib.mixkvq_decode_step.argtypes = [vp, vp, vp, i64p, vp, vp, vp, C.c_float, i32, vp]
     lib.mixkvq_set_timing_events.argtypes = [vp, vp, vp]
     lib.mixkvq_decode_path.argtypes = [vp]
+    i64, i32p = C.c_int64, C.POINTER(C.c_int32)
+    lib.mixkvq_chunk_workspace.argtypes = [vp, i32, i32p]
+    lib.mixkvq_chunk_attention.argtypes = [vp, vp, i64p, vp, vp, i64p, i32, i32p, vp, i64p, vp, C.c_float, i32, vp, i64, vp]
+    lib.mixkvq_verify_workspace.argtypes = [i32, i32]
+    lib.mixkvq_verify_draft.argtypes = [i32, i32, i32, vp, i64p, vp, i64p, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.mixkvq_strerror.argtypes = [i32]
     lib.mixkvq_strerror.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("mixkvq_cache_destroy", "mixkvq_strerror"):
-            getattr(lib, name).restype = i32
+            getattr(lib, name).restype = i64 if name.endswith("_workspace") else i32
     _lib = lib
     return lib
 
@@ -109,6 +115,26 @@ def _stream_ptr(stream) -> int:
     if stream is None:
         return _raw_stream(_device()) if _raw_stream and _device else torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream
+
+
+class _on:
+    """The tensors' device and the given stream (None: the current one) as the current ones, where they are not already: what a
+    call allocates then belongs to the stream that uses it."""
+
+    def __init__(self, device, stream):
+        self.ctx = []
+        if torch.cuda.current_device() != (device.index or 0):
+            self.ctx.append(torch.cuda.device(device))
+        if stream is not None:
+            self.ctx.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.ctx:
+            c.__enter__()
+
+    def __exit__(self, *exc):
+        for c in reversed(self.ctx):
+            c.__exit__(*exc)
 
 
 _I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
@@ -320,6 +346,38 @@ class Cache:
                                            int(bool(accumulate_q)), _stream_ptr(stream)))
         return out, lse
 
+    def chunk_attention(self, q, k_new, v_new, n_seq=None, out=None, lse=None, scale=0.0, accumulate_q=False, workspace=None,
+                        stream=None):
+        """q: fp16 [B, Hq, n, D]; k_new, v_new: fp16 [B, Hkv, n, D] with equal strides (unit channel stride, the others any
+        multiples of 8).  n_seq: new tokens of each sequence (host integers) or None.  Attention of the n new tokens over the
+        cache and, causally, over themselves; nothing is appended.  Returns (out [B, Hq, n, D], strides as q's unless given, and
+        lse fp32 [B, Hq, n]); rows behind a sequence's n_seq are left as they are."""
+        B, Hq, n, D = q.shape
+        cfg = self.cfg
+        assert (B, Hq, D) == (cfg.B, cfg.Hq, cfg.D) and k_new.shape == (B, cfg.Hkv, n, D) == v_new.shape
+        dt = torch.bfloat16 if cfg.in_dtype else torch.float16
+        assert k_new.stride() == v_new.stride() and q.dtype == k_new.dtype == v_new.dtype == dt
+        counts = None
+        if n_seq is not None:
+            assert len(n_seq) == B
+            counts = (C.c_int32 * B)(*n_seq)
+        with _on(self.device, stream):
+            if out is None:
+                out = torch.empty_like(q)
+            if lse is None:
+                lse = torch.empty((B, Hq, n), dtype=torch.float32, device=self.device)
+            assert out.shape == q.shape and out.dtype == dt
+            assert lse.shape == (B, Hq, n) and lse.dtype == torch.float32 and lse.is_contiguous()
+            need = self.lib.mixkvq_chunk_workspace(self.handle, n, counts)
+            _check(min(need, 0))
+            if workspace is None and need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+            _check(self.lib.mixkvq_chunk_attention(self.handle, q.data_ptr(), _strides3(q), k_new.data_ptr(), v_new.data_ptr(),
+                                                   _strides3(k_new), n, counts, out.data_ptr(), _strides3(out), lse.data_ptr(),
+                                                   float(scale), int(bool(accumulate_q)), wp, wn, _stream_ptr(stream)))
+        return out, lse
+
     def set_timing_events(self, start_event, stop_event):
         """start_event, stop_event: raw hipEvent_t handles (ints) or None, None."""
         _check(self.lib.mixkvq_set_timing_events(self.handle, start_event, stop_event))
@@ -356,3 +414,39 @@ class Cache:
         P = self.cfg.B * self.cfg.Hkv
         a = self.qacc[:P * (self.cfg.D + 1) * 8].view(torch.int64)
         return a[:P * self.cfg.D].view(P, self.cfg.D), a[P * self.cfg.D:]
+
+
+def verify_draft(p_target, draft, u_accept, u_next, p_draft=None, n_seq=None, n_accepted=None, tokens=None, workspace=None, stream=None):
+    """p_target: fp32 [B, n + 1, V] (any strides but the last); draft: int32 [B, n]; u_accept: fp32 [B, n]; u_next: fp32 [B];
+    p_draft: fp32 [B, n, V] or None (looked-up drafts); n_seq: int32 [B] on the device or None.  Returns (n_accepted int32 [B],
+    tokens int32 [B, n + 1]: the drafts that stay, the token that follows, then -1)."""
+    lib = load_library()
+    B, n1, V = p_target.shape
+    n = n1 - 1
+    assert p_target.is_cuda and p_target.dtype == torch.float32 and p_target.stride(2) == 1
+    assert draft.shape == (B, n) == u_accept.shape and draft.dtype == torch.int32 and u_accept.dtype == torch.float32
+    assert draft.is_contiguous() and u_accept.is_contiguous()
+    assert u_next.shape == (B,) and u_next.dtype == torch.float32 and u_next.is_contiguous()
+    if p_draft is not None:
+        assert p_draft.shape == (B, n, V) and p_draft.dtype == torch.float32 and (p_draft.numel() == 0 or p_draft.stride(2) == 1)
+    if n_seq is not None:
+        assert n_seq.shape == (B,) and n_seq.dtype == torch.int32 and n_seq.is_contiguous() and n_seq.is_cuda
+    device = p_target.device
+    with _on(device, stream):
+        if n_accepted is None:
+            n_accepted = torch.empty(B, dtype=torch.int32, device=device)
+        if tokens is None:
+            tokens = torch.empty((B, n1), dtype=torch.int32, device=device)
+        assert n_accepted.shape == (B,) and n_accepted.dtype == torch.int32 and n_accepted.is_contiguous()
+        assert tokens.shape == (B, n1) and tokens.dtype == torch.int32 and tokens.is_contiguous()
+        need = lib.mixkvq_verify_workspace(B, V)
+        _check(min(need, 0))
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        _check(lib.mixkvq_verify_draft(B, n, V, p_target.data_ptr(), _I64x2(p_target.stride(0), p_target.stride(1)),
+                                       None if p_draft is None else p_draft.data_ptr(),
+                                       None if p_draft is None else _I64x2(p_draft.stride(0), p_draft.stride(1)),
+                                       draft.data_ptr(), None if n_seq is None else n_seq.data_ptr(), u_accept.data_ptr(),
+                                       u_next.data_ptr(), n_accepted.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
+                                       workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return n_accepted, tokens

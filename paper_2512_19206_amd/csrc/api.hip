@@ -4,22 +4,17 @@
 #include <new>
 #include <stdio.h>
 #include <string.h>
-#include "mixkvq_internal.h"
+#include "cache_state.h"
 
 namespace mixkvq {
 
 static thread_local char g_hip_msg[256] = "no HIP error recorded";
 
-static int hip_fail(hipError_t e) {
+int hip_fail(hipError_t e) {
   snprintf(g_hip_msg, sizeof(g_hip_msg), "HIP error %d: %s", (int)e, hipGetErrorString(e));
   (void)hipGetLastError();
   return MIXKVQ_EHIP;
 }
-#define MIXKVQ_TRY_HIP(expr)                          \
-  do {                                                \
-    hipError_t e__ = (expr);                          \
-    if (e__ != hipSuccess) return hip_fail(e__);      \
-  } while (0)
 
 static inline int al16(int n) { return (n + 15) / 16 * 16; }
 
@@ -91,22 +86,6 @@ static inline uint64_t al256(uint64_t n) { return (n + 255) / 256 * 256; }
 }  // namespace mixkvq
 
 using namespace mixkvq;
-
-struct SeqState {
-  int64_t n_quant;   // quantized tokens
-  int32_t n_res;     // tokens in the residual window
-  int32_t n_sink;    // tokens in the sink
-  bool operator==(const SeqState& o) const { return n_quant == o.n_quant && n_res == o.n_res && n_sink == o.n_sink; }
-};
-
-struct mixkvq_cache {
-  CacheView v;       // v.cfg.R is the number of tokens per RECORD (what the kernels work on): rec_tokens()
-  int32_t Rw;        // the residual length R of the configuration: window size and flush unit, Rw / v.cfg.R records per block
-  SeqState* seq;     // [B]: every sequence has its own counts (they are equal while the batch runs in lock-step)
-  hipEvent_t ev_start = nullptr, ev_stop = nullptr;   // optional timing of the split kernel
-  int last_path = MIXKVQ_PATH_NONE;                   // kernel of the last attention launch
-  bool tickets_clear = false;                         // the ticket words were set to 0 once
-};
 
 namespace mixkvq {
 
@@ -205,7 +184,7 @@ static int append_range(mixkvq_cache* c, int b0, int nb, const __half* k_new, co
   return MIXKVQ_OK;
 }
 
-static bool lock_step(const mixkvq_cache* c) {
+bool lock_step(const mixkvq_cache* c) {
   for (int b = 1; b < c->v.cfg.B; ++b)
     if (!(c->seq[b] == c->seq[0])) return false;
   return true;
@@ -632,7 +611,7 @@ const char* mixkvq_strerror(int code) {
     case MIXKVQ_EHIP: return mixkvq::g_hip_msg;
     case MIXKVQ_ENOMEM: return "host allocation failed";
     case MIXKVQ_EEMPTY: return "the cache holds no token";
-    case MIXKVQ_ESCRATCH: return "the split-K partials of this launch exceed the library's built-in scratch buffer (8 MiB)";
+    case MIXKVQ_ESCRATCH: return "the launch needs more scratch memory than the library's built-in buffer (8 MiB) or the caller's workspace has";
     case MIXKVQ_ERAGGED: return "the sequences of the batch hold different numbers of tokens: ask per sequence";
     default: return "unknown mixkvq error code";
   }
