@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmixkvq.so")
 SOURCES = ["api.hip", "select_kernels.hip", "quantize_kernels.hip", "decode_kernels.hip", "decode_mfma.hip", "decode_mfma_any_lengths.hip",
-           "chunk_api.hip", "chunk_kernels.hip", "verify_kernels.hip",
+           "chunk_api.hip", "chunk_kernels.hip", "chunk_few_1.hip", "chunk_few_2.hip", "chunk_few_3.hip", "verify_kernels.hip",
            "decode_mfma_generic_plain.hip", "decode_mfma_generic_g32.hip", "decode_mfma_generic_rh.hip"]
 OBJ_DIR = os.path.join(HERE, "_build")      # object files (git-ignored)
 

@@ -34,8 +34,10 @@ struct ChunkArgs {
   float* part;                         // [unit][rows][kD], then [unit][rows][2]: partial sums, maxima and sums of weights
 };
 
-// Query rows of one workgroup: its eight wavefronts stand in 2, 4 or 8 groups of 32 rows.
-hipError_t launch_chunk(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, int row_groups, bool split, hipStream_t s);
+// Two kernels: the tile kernel (chunk_kernels.hip; 64, 128 or 256 query rows to a workgroup, any configuration) and the one for
+// few rows (chunk_few.h; 16, 32 or 48, the record layouts that chunk_few_fits takes).
+bool chunk_few_fits(const CacheView& v);
+hipError_t launch_chunk(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool few, int rows, bool split, hipStream_t s);
 hipError_t launch_chunk_books(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, hipStream_t s);   // |q| of the chunk
 int chunk_tile_records(const CacheView& v);      // records of one tile
 

@@ -1,5 +1,6 @@
 // mixkvq_chunk_attention: argument checks, and how a launch's work is cut into workgroups.
 #include <math.h>
+#include <stdlib.h>
 #include "cache_state.h"
 #include "chunk.h"
 
@@ -12,36 +13,40 @@ constexpr int kChunkMaxNew = 1 << 20;
 
 static int div_up(int a, int b) { return (a + b - 1) / b; }
 
-// How a call is cut: groups of 32 query rows per workgroup, tiles of tokens per split.
-struct ChunkPlan { int row_groups, chain; };
+// How a call is cut: the kernel, the query rows of a workgroup, and how much of a pair's tokens one workgroup takes.
+struct ChunkPlan { bool few; int rows, chain; };
 
 static int n_new_of(const int32_t* n_seq, int n_max, int b) { return n_seq ? n_seq[b] : n_max; }
 
-// Tiles that the longest row tile of sequence b walks over.
-static int chunk_tiles(const mixkvq_cache* c, int tile_rec, int b, int n) {
+// What a workgroup without splits would do one after the other for sequence b: tiles, or with few rows slices of each of its
+// eight wavefronts.
+static int chunk_steps(const mixkvq_cache* c, bool few, int b, int n) {
   const SeqState& st = c->seq[b];
-  return div_up((int)(st.n_quant / c->v.cfg.R), tile_rec) + div_up(st.n_sink + st.n_res, kChunkTile) + div_up(n, kChunkTile);
+  const int rec = (int)(st.n_quant / c->v.cfg.R), rows = st.n_sink + st.n_res;
+  if (few) return div_up(rec * (c->v.cfg.R / 32) + div_up(rows, 32) + div_up(n, 32), 8);
+  return div_up(rec, chunk_tile_records(c->v)) + div_up(rows, kChunkTile) + div_up(n, kChunkTile);
 }
 
-static int splits_of(int tiles, int chain) {
-  const int s = div_up(tiles, chain);
+static int splits_of(int steps, int chain) {
+  const int s = div_up(steps, chain);
   return s > kChunkMaxSplits ? kChunkMaxSplits : s;
 }
 
 static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
   const mixkvq_config& cfg = c->v.cfg;
-  const int tile_rec = chunk_tile_records(c->v);
   int most = 0;
   for (int b = 0; b < cfg.B; ++b) most = n_new_of(n_seq, n_max, b) > most ? n_new_of(n_seq, n_max, b) : most;
   ChunkPlan pl{};
   const int rows = most * c->v.g;
-  pl.row_groups = rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
-  // The splits' length that takes the least time: rounds of workgroups times what one does, its tiles and a constant part,
-  // and more where the splits have to be merged.
+  static const int few_rows = getenv("MIXKVQ_FEW") ? atoi(getenv("MIXKVQ_FEW")) : 96;
+  pl.few = rows <= few_rows && chunk_few_fits(c->v);
+  if (pl.few) pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 48;
+  else pl.rows = rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  // The splits' length that takes the least time: rounds of workgroups times what one does, its steps and a constant part, and
+  // more where the splits have to be merged.
   int longest = 1;
   for (int b = 0; b < cfg.B; ++b) {
-    const int n = n_new_of(n_seq, n_max, b);
-    const int t = n ? chunk_tiles(c, tile_rec, b, n) : 0;
+    const int n = n_new_of(n_seq, n_max, b), t = n ? chunk_steps(c, pl.few, b, n) : 0;
     longest = t > longest ? t : longest;
   }
   double best = 0;
@@ -52,7 +57,7 @@ static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_s
     int64_t units = 0;
     for (int b = 0; b < cfg.B; ++b) {
       const int n = n_new_of(n_seq, n_max, b);
-      if (n) units += (int64_t)cfg.Hkv * div_up(n * c->v.g, 32 * pl.row_groups) * splits_of(chunk_tiles(c, tile_rec, b, n), chain);
+      if (n) units += (int64_t)cfg.Hkv * div_up(n * c->v.g, pl.rows) * splits_of(chunk_steps(c, pl.few, b, n), chain);
     }
     const double t = (double)((units + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain + 3) + (s > 1 ? 4 : 0);
     if (s == 1 || t < best) {
@@ -66,17 +71,16 @@ static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_s
 // Sequences [b0, b0 + n) of the call as one launch.
 static ChunkLaunch fill_launch(const mixkvq_cache* c, const ChunkPlan& pl, int b0, int n, int n_max, const int32_t* n_seq, bool* split) {
   ChunkLaunch l{};
-  const int tile_rec = chunk_tile_records(c->v);
   l.b0 = b0;
   l.n_seq = n;
-  l.tile_rec = tile_rec;
+  l.tile_rec = chunk_tile_records(c->v);
   int units = 0, same = -1;
   *split = false;
   for (int i = 0; i < n; ++i) {
     const SeqState& st = c->seq[b0 + i];
     const int nn = n_new_of(n_seq, n_max, b0 + i);
-    const int splits = nn ? splits_of(chunk_tiles(c, tile_rec, b0 + i, nn), pl.chain) : 1;
-    const int u = c->v.cfg.Hkv * div_up(nn * c->v.g, 32 * pl.row_groups) * splits;
+    const int splits = nn ? splits_of(chunk_steps(c, pl.few, b0 + i, nn), pl.chain) : 1;
+    const int u = c->v.cfg.Hkv * div_up(nn * c->v.g, pl.rows) * splits;
     l.n_rec[i] = (int)(st.n_quant / c->v.cfg.R);
     l.n_new[i] = nn;
     l.rows_splits[i] = (uint32_t)(st.n_sink + st.n_res) | (uint32_t)splits << 16;
@@ -90,9 +94,7 @@ static ChunkLaunch fill_launch(const mixkvq_cache* c, const ChunkPlan& pl, int b
   return l;
 }
 
-static size_t launch_part_bytes(const ChunkLaunch& l, const ChunkPlan& pl) {
-  return (size_t)l.n_units * 32 * pl.row_groups * (kD + 2) * sizeof(float);
-}
+static size_t launch_part_bytes(const ChunkLaunch& l, const ChunkPlan& pl) { return (size_t)l.n_units * pl.rows * (kD + 2) * sizeof(float); }
 
 static int check_counts(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
   if (!c || n_max < 0 || n_max > kChunkMaxNew) return MIXKVQ_EINVAL;
@@ -100,7 +102,7 @@ static int check_counts(const mixkvq_cache* c, int n_max, const int32_t* n_seq) 
     for (int b = 0; b < c->v.cfg.B; ++b)
       if (n_seq[b] < 0 || n_seq[b] > n_max) return MIXKVQ_EINVAL;
   // unit numbers are 32-bit
-  if ((int64_t)c->v.P * ((int64_t)n_max * c->v.g / 64 + 1) * kChunkMaxSplits >= 1ll << 31) return MIXKVQ_EINVAL;
+  if ((int64_t)c->v.P * ((int64_t)n_max * c->v.g / 16 + 1) * kChunkMaxSplits >= 1ll << 31) return MIXKVQ_EINVAL;
   return MIXKVQ_OK;
 }
 
@@ -167,7 +169,7 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
     bool split;
     const ChunkLaunch l = fill_launch(c, pl, b0, n, n_new, n_seq, &split);
     if (l.n_units == 0) continue;
-    MIXKVQ_TRY_HIP(launch_chunk(c->v, a, l, pl.row_groups, split, s));
+    MIXKVQ_TRY_HIP(launch_chunk(c->v, a, l, pl.few, pl.rows, split, s));
     if (accumulate_q) MIXKVQ_TRY_HIP(launch_chunk_books(c->v, a, l, s));
   }
   return MIXKVQ_OK;

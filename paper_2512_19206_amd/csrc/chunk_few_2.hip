@@ -1,0 +1,8 @@
+// The kernel for few query rows with up to 32 rows to a workgroup.
+#include "chunk_few.h"
+
+namespace mixkvq {
+hipError_t start_chunk_few_2(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s) {
+  return few::start_any<2>(v, a, l, split, s);
+}
+}  // namespace mixkvq

@@ -629,14 +629,31 @@ static int most_rows(const CacheView& v, const ChunkLaunch& l) {
   return most * v.g;
 }
 
-hipError_t launch_chunk(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, int row_groups, bool split, hipStream_t s) {
-  if (row_groups == 2) start_chunk<2>(v, a, l, split, s);
-  else if (row_groups == 4) start_chunk<4>(v, a, l, split, s);
-  else start_chunk<8>(v, a, l, split, s);
-  hipError_t e = hipGetLastError();
+hipError_t start_chunk_few_1(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s);
+hipError_t start_chunk_few_2(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s);
+hipError_t start_chunk_few_3(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s);
+
+// Slices of 32 tokens inside one record and one key group; two to four steps of 32 channel places with nothing but 2-bit codes
+// and one with the rest, at most one step of fp16 places.
+bool chunk_few_fits(const CacheView& v) {
+  const int octets = v.lay.NLp / 8 + v.lay.W4;
+  return v.cfg.R % 32 == 0 && v.cfg.Gk % 32 == 0 && v.lay.NVG <= 4 && v.cfg.k16 <= 32 &&
+         (v.lay.NLp == 128 ? octets <= 20 : v.lay.NLp >= 96 && octets <= 16);
+}
+
+hipError_t launch_chunk(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool few, int rows, bool split, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (few) {
+    e = rows == 16 ? start_chunk_few_1(v, a, l, split, s) : rows == 32 ? start_chunk_few_2(v, a, l, split, s) : start_chunk_few_3(v, a, l, split, s);
+  } else {
+    if (rows == 64) start_chunk<2>(v, a, l, split, s);
+    else if (rows == 128) start_chunk<4>(v, a, l, split, s);
+    else start_chunk<8>(v, a, l, split, s);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || !split) return e;
   const int per_pair = (most_rows(v, l) + 15) / 16;
-  chunk_merge_kernel<<<per_pair * l.n_seq * v.cfg.Hkv, 256, 0, s>>>(v, a, l, 32 * row_groups, per_pair);
+  chunk_merge_kernel<<<per_pair * l.n_seq * v.cfg.Hkv, 256, 0, s>>>(v, a, l, rows, per_pair);
   return hipGetLastError();
 }
 
