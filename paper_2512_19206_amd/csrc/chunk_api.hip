@@ -1,6 +1,5 @@
 // mixkvq_chunk_attention: argument checks, and how a launch's work is cut into workgroups.
 #include <math.h>
-#include <stdlib.h>
 #include "cache_state.h"
 #include "chunk.h"
 
@@ -10,6 +9,7 @@ namespace mixkvq {
 
 constexpr int kChunkUnitsAtOnce = 256;      // one workgroup to a compute unit (its tiles fill the LDS)
 constexpr int kChunkMaxNew = 1 << 20;
+constexpr int kFewRows = 96;                // query rows up to which the kernel for few rows is taken
 
 static int div_up(int a, int b) { return (a + b - 1) / b; }
 
@@ -38,9 +38,8 @@ static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_s
   for (int b = 0; b < cfg.B; ++b) most = n_new_of(n_seq, n_max, b) > most ? n_new_of(n_seq, n_max, b) : most;
   ChunkPlan pl{};
   const int rows = most * c->v.g;
-  static const int few_rows = getenv("MIXKVQ_FEW") ? atoi(getenv("MIXKVQ_FEW")) : 96;
-  pl.few = rows <= few_rows && chunk_few_fits(c->v);
-  if (pl.few) pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 48;
+  pl.few = rows <= kFewRows && chunk_few_fits(c->v);
+  if (pl.few) pl.rows = rows <= 16 ? 16 : rows <= 32 || chunk_few_rows(c->v) == 32 ? 32 : 48;
   else pl.rows = rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   // The splits' length that takes the least time: rounds of workgroups times what one does, its steps and a constant part, and
   // more where the splits have to be merged.
@@ -68,33 +67,59 @@ static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_s
   return pl;
 }
 
-// Sequences [b0, b0 + n) of the call as one launch.
-static ChunkLaunch fill_launch(const mixkvq_cache* c, const ChunkPlan& pl, int b0, int n, int n_max, const int32_t* n_seq, bool* split) {
-  ChunkLaunch l{};
-  l.b0 = b0;
-  l.n_seq = n;
-  l.tile_rec = chunk_tile_records(c->v);
-  int units = 0, same = -1;
-  *split = false;
-  for (int i = 0; i < n; ++i) {
-    const SeqState& st = c->seq[b0 + i];
-    const int nn = n_new_of(n_seq, n_max, b0 + i);
-    const int splits = nn ? splits_of(chunk_steps(c, pl.few, b0 + i, nn), pl.chain) : 1;
-    const int u = c->v.cfg.Hkv * div_up(nn * c->v.g, pl.rows) * splits;
-    l.n_rec[i] = (int)(st.n_quant / c->v.cfg.R);
-    l.n_new[i] = nn;
-    l.rows_splits[i] = (uint32_t)(st.n_sink + st.n_res) | (uint32_t)splits << 16;
-    l.first_unit[i] = units;
-    units += u;
-    same = same == -1 ? u : same == u ? u : 0;
-    *split = *split || splits > 1;
+// Sequences [b0, b0 + n) of the call as one launch (counts that differ in *c).  How many sequences a launch takes is up to the
+// caller (next_launch).
+struct ChunkLaunch { int b0, n, units, row_tiles, most; bool equal, split; };
+
+static int units_of(const mixkvq_cache* c, const ChunkPlan& pl, int b, int n) { return n ? splits_of(chunk_steps(c, pl.few, b, n), pl.chain) : 0; }
+
+static ChunkLaunch next_launch(const mixkvq_cache* c, const ChunkPlan& pl, int b0, int n_max, const int32_t* n_seq) {
+  ChunkLaunch l{b0, 0, 0, 0, 0, true, false};
+  const int B = c->v.cfg.B;
+  while (b0 + l.n < B) {
+    const int b = b0 + l.n, n = n_new_of(n_seq, n_max, b), u = units_of(c, pl, b, n);
+    const bool equal = l.equal && c->seq[b] == c->seq[b0] && n == n_new_of(n_seq, n_max, b0);
+    if (!equal && (l.n >= kChunkSeqs || l.units + u > kChunkUnits)) break;
+    l.equal = equal;
+    l.units += u;
+    l.split = l.split || u > 1;
+    l.most = n > l.most ? n : l.most;
+    ++l.n;
   }
-  l.n_units = units;
-  l.same_units = same > 0 ? same : 0;
+  l.row_tiles = div_up(l.most * c->v.g, pl.rows);
   return l;
 }
 
-static size_t launch_part_bytes(const ChunkLaunch& l, const ChunkPlan& pl) { return (size_t)l.n_units * pl.rows * (kD + 2) * sizeof(float); }
+static void fill_launch(const mixkvq_cache* c, const ChunkPlan& pl, const ChunkLaunch& l, int n_max, const int32_t* n_seq, ChunkArgs* a, ChunkCounts* counts) {
+  a->b0 = l.b0;
+  a->row_tiles = l.row_tiles;
+  a->split = l.split;
+  int units = 0;
+  for (int i = 0; i < (l.equal ? 1 : l.n); ++i) {
+    const SeqState& st = c->seq[l.b0 + i];
+    const int n = n_new_of(n_seq, n_max, l.b0 + i), u = units_of(c, pl, l.b0 + i, n);
+    const int n_rec = (int)(st.n_quant / c->v.cfg.R), n_fp16 = st.n_sink + st.n_res;
+    if (l.equal) {
+      a->n_rec = n_rec;
+      a->n_fp16 = n_fp16;
+      a->n_new = n;
+      a->n_splits = u;
+      return;
+    }
+    counts->n_rec[i] = n_rec;
+    counts->n_new[i] = n;
+    counts->rows_splits[i] = (uint32_t)n_fp16 | (uint32_t)u << 16;
+    counts->first[i] = units;
+    for (int k = 0; k < u; ++k, ++units) {
+      uint32_t& word = counts->owner[units >> 2];
+      word = (units & 3) ? word | (uint32_t)i << (8 * (units & 3)) : (uint32_t)i;
+    }
+  }
+}
+
+static size_t part_bytes(const mixkvq_cache* c, const ChunkLaunch& l, const ChunkPlan& pl) {
+  return l.split ? (size_t)l.units * c->v.cfg.Hkv * l.row_tiles * pl.rows * (kD + 2) * sizeof(float) : 0;
+}
 
 static int check_counts(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
   if (!c || n_max < 0 || n_max > kChunkMaxNew) return MIXKVQ_EINVAL;
@@ -122,12 +147,11 @@ int64_t mixkvq_chunk_workspace(const mixkvq_cache* c, int32_t n_new, const int32
   if (rc != MIXKVQ_OK) return rc;
   const ChunkPlan pl = plan_chunk(c, n_new, n_seq);
   size_t most = 0;
-  for (int b0 = 0; b0 < c->v.cfg.B; b0 += kChunkSeqs) {
-    const int n = c->v.cfg.B - b0 < kChunkSeqs ? c->v.cfg.B - b0 : kChunkSeqs;
-    bool split;
-    const ChunkLaunch l = fill_launch(c, pl, b0, n, n_new, n_seq, &split);
-    const size_t bytes = split ? launch_part_bytes(l, pl) : 0;
+  for (int b0 = 0; b0 < c->v.cfg.B;) {
+    const ChunkLaunch l = next_launch(c, pl, b0, n_new, n_seq);
+    const size_t bytes = part_bytes(c, l, pl);
     most = bytes > most ? bytes : most;
+    b0 += l.n;
   }
   return (int64_t)most;
 }
@@ -142,6 +166,7 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
   if (!rows_ok(q, q_strides) || !rows_ok(k_new, kv_strides) || !rows_ok(v_new, kv_strides) || !rows_ok(out, out_strides)) return MIXKVQ_EINVAL;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)kD);
   if (!(scale < INFINITY)) return MIXKVQ_EINVAL;
+  if (kv_strides[2] != (int32_t)kv_strides[2]) return MIXKVQ_EINVAL;      // (row numbers times it are formed by a 32-bit multiply)
   const mixkvq_config& cfg = c->v.cfg;
   if ((workspace && ((uintptr_t)workspace & 15u)) || workspace_bytes < 0) return MIXKVQ_EINVAL;
   const ChunkPlan pl = plan_chunk(c, n_new, n_seq);
@@ -158,19 +183,56 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
   a.scale = scale;
   a.part = (float*)workspace;
   const hipStream_t s = (hipStream_t)stream;
-  for (int b0 = 0; b0 < cfg.B; b0 += kChunkSeqs) {      // everything is checked before the first launch
-    const int n = cfg.B - b0 < kChunkSeqs ? cfg.B - b0 : kChunkSeqs;
-    bool split;
-    const ChunkLaunch l = fill_launch(c, pl, b0, n, n_new, n_seq, &split);
-    if (split && (!workspace || launch_part_bytes(l, pl) > (size_t)workspace_bytes)) return MIXKVQ_ESCRATCH;
+  const CacheView& v = c->v;
+  const Layout& lay = v.lay;
+  a.blocks = v.blocks;
+  a.table = v.table;
+  a.res_k = v.res_k;
+  a.res_v = v.res_v;
+  a.NB = v.NB;
+  a.RW = v.RW;
+  a.Hkv = cfg.Hkv;
+  a.Hq = cfg.Hq;
+  a.g = v.g;
+  a.bf16 = cfg.in_dtype != 0;
+  a.R = cfg.R;
+  a.Gk = cfg.Gk;
+  a.Gv = cfg.Gv;
+  a.k4 = cfg.k4;
+  a.k16 = cfg.k16;
+  a.rec_bytes = lay.rec_bytes;
+  a.tile_rec = chunk_tile_records(v);
+  a.NLp = lay.NLp;
+  a.Wlo = lay.Wlo;
+  a.W4 = lay.W4;
+  a.NVG = lay.NVG;
+  a.interleave = lay.v_interleave;
+  a.off_idx = lay.off_idx;
+  a.off_kmax = lay.off_kmax;
+  a.off_klo_s = lay.off_klo_s;
+  a.off_klo_z = lay.off_klo_z;
+  a.off_k4_s = lay.off_k4_s;
+  a.off_k4_z = lay.off_k4_z;
+  a.off_klo = lay.off_klo;
+  a.off_k4 = lay.off_k4;
+  a.off_k16 = lay.off_k16;
+  a.off_v = lay.off_v;
+  a.off_v_s = lay.off_v_s;
+  a.off_v_z = lay.off_v_z;
+  for (int b0 = 0; b0 < cfg.B;) {      // everything is checked before the first launch
+    const ChunkLaunch l = next_launch(c, pl, b0, n_new, n_seq);
+    const size_t bytes = part_bytes(c, l, pl);
+    if (bytes && (!workspace || bytes > (size_t)workspace_bytes)) return MIXKVQ_ESCRATCH;
+    b0 += l.n;
   }
-  for (int b0 = 0; b0 < cfg.B; b0 += kChunkSeqs) {
-    const int n = cfg.B - b0 < kChunkSeqs ? cfg.B - b0 : kChunkSeqs;
-    bool split;
-    const ChunkLaunch l = fill_launch(c, pl, b0, n, n_new, n_seq, &split);
-    if (l.n_units == 0) continue;
-    MIXKVQ_TRY_HIP(launch_chunk(c->v, a, l, pl.few, pl.rows, split, s));
-    if (accumulate_q) MIXKVQ_TRY_HIP(launch_chunk_books(c->v, a, l, s));
+  for (int b0 = 0; b0 < cfg.B;) {
+    const ChunkLaunch l = next_launch(c, pl, b0, n_new, n_seq);
+    b0 += l.n;
+    if (l.units == 0) continue;
+    ChunkCounts counts;
+    fill_launch(c, pl, l, n_new, n_seq, &a, &counts);
+    MIXKVQ_TRY_HIP(launch_chunk(a, l.equal ? nullptr : &counts, l.units, l.n, pl.few, pl.rows, s));
+    if (accumulate_q) MIXKVQ_TRY_HIP(launch_chunk_books(v, a, l.equal ? nullptr : &counts, l.n, l.most, s));
   }
   return MIXKVQ_OK;
 }

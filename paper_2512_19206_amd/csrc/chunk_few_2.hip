@@ -2,7 +2,5 @@
 #include "chunk_few.h"
 
 namespace mixkvq {
-hipError_t start_chunk_few_2(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s) {
-  return few::start_any<2>(v, a, l, split, s);
-}
+hipError_t start_chunk_few_2(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s) { return few::start_any<2>(a, c, units, s); }
 }  // namespace mixkvq

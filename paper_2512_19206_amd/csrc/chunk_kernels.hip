@@ -7,6 +7,7 @@
 // O^T = V^T P^T, 32 tokens (channels) by 32 rows at a time: a lane then holds one row's scores, so that the softmax needs
 // one exchange between the two halves of the wavefront, and the weights P go into the second product from the registers in
 // which the first one left them.
+#include <type_traits>
 #include "chunk.h"
 
 namespace mixkvq {
@@ -178,22 +179,21 @@ __device__ __forceinline__ void attend(unsigned char* lds, int keys, int values,
 }
 
 // Dequantizes the staged tile's keys into `keys` (a row per channel).  Threads 0 .. 255; threads 256 .. 511 do the values.
-__device__ __forceinline__ void unpack_keys(unsigned char* lds, const CacheView& cv, int keys, const unsigned short* map, int n_tok) {
-  const Layout& lay = cv.lay;
-  const int Rr = cv.cfg.R, tid = threadIdx.x;
+__device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs& a, int keys, const unsigned short* map, int n_tok) {
+  const int Rr = a.R, tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   {  // 2-bit channels: eight tokens of the eight even or odd channels of a word
     const int odd = wave & 1, tg = (wave >> 1) * 8 + (lane & 7), w = lane >> 3, t = tg * 8;
-    if (w < lay.Wlo && t < n_tok) {
-      const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * lay.rec_bytes;
-      const int words = raw + lay.off_klo + (tin * lay.Wlo + w) * 4;
+    if (w < a.Wlo && t < n_tok) {
+      const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
+      const int words = raw + a.off_klo + (tin * a.Wlo + w) * 4;
       const unsigned pick = odd ? 0x07060302u : 0x05040100u, twice = odd ? 0x03020302u : 0x01000100u;
       unsigned x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * lay.Wlo * 4),
-                                     *reinterpret_cast<const unsigned*>(lds + words + 2 * i * lay.Wlo * 4), pick);
-      const int sc = raw + lay.off_klo_s + ((tin / cv.cfg.Gk) * lay.NLp + 16 * w) * 2, zc = sc + lay.off_klo_z - lay.off_klo_s;
+        x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * a.Wlo * 4),
+                                     *reinterpret_cast<const unsigned*>(lds + words + 2 * i * a.Wlo * 4), pick);
+      const int sc = raw + a.off_klo_s + ((tin / a.Gk) * a.NLp + 16 * w) * 2, zc = sc + a.off_klo_z - a.off_klo_s;
       const unsigned* s = reinterpret_cast<const unsigned*>(lds + sc);
       const unsigned* z = reinterpret_cast<const unsigned*>(lds + zc);
       const unsigned* at = reinterpret_cast<const unsigned*>(map + rec * kD + 16 * w);
@@ -211,21 +211,21 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const CacheView&
     }
   }
   // Side tiers: their channels stand in the record's list, an unused entry (255) goes to the row that nobody reads.
-  const int k4 = cv.cfg.k4, k16 = cv.cfg.k16;
-  for (int u = tid; u < lay.W4 * 32; u += 256) {      // four bits: eight tokens of the four even or odd channels of a word
+  const int k4 = a.k4, k16 = a.k16;
+  for (int u = tid; u < a.W4 * 32; u += 256) {      // four bits: eight tokens of the four even or odd channels of a word
     const int odd = u & 1, tg = (u >> 1) & 15, w = u >> 5, t = tg * 8;
     if (t >= n_tok) continue;
-    const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * lay.rec_bytes;
-    const int words = raw + lay.off_k4 + (tin * lay.W4 + w) * 4;
+    const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
+    const int words = raw + a.off_k4 + (tin * a.W4 + w) * 4;
     const unsigned pick = odd ? 0x07060302u : 0x05040100u, twice = odd ? 0x03020302u : 0x01000100u;
     unsigned x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * lay.W4 * 4),
-                                   *reinterpret_cast<const unsigned*>(lds + words + 2 * i * lay.W4 * 4), pick);
-    const unsigned* s = reinterpret_cast<const unsigned*>(lds + raw + lay.off_k4_s + ((tin / cv.cfg.Gk) * k4 + 8 * w) * 2);
-    const unsigned* z = reinterpret_cast<const unsigned*>(lds + raw + lay.off_k4_z + ((tin / cv.cfg.Gk) * k4 + 8 * w) * 2);
-    const unsigned char* list = lds + raw + lay.off_idx + k16 + 8 * w + odd;
+      x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * a.W4 * 4),
+                                   *reinterpret_cast<const unsigned*>(lds + words + 2 * i * a.W4 * 4), pick);
+    const unsigned* s = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_s + ((tin / a.Gk) * k4 + 8 * w) * 2);
+    const unsigned* z = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_z + ((tin / a.Gk) * k4 + 8 * w) * 2);
+    const unsigned char* list = lds + raw + a.off_idx + k16 + 8 * w + odd;
 #define MIXKVQ_CHANNEL(I)                                                                                                  \
   {                                                                                                                        \
     const h2 s2 = as_h2(__builtin_amdgcn_perm(s[I], s[I], twice)), z2 = as_h2(__builtin_amdgcn_perm(z[I], z[I], twice));   \
@@ -240,15 +240,15 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const CacheView&
   for (int u = tid; u < k16 * 8; u += 256) {      // fp16: eight tokens of two neighbouring entries
     const int tg = u & 15, e = (u >> 4) * 2, t = tg * 8;
     if (t >= n_tok) continue;
-    const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * lay.rec_bytes;
-    const unsigned char* src = lds + raw + lay.off_k16 + (tin * k16 + e) * 2;
+    const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
+    const unsigned char* src = lds + raw + a.off_k16 + (tin * k16 + e) * 2;
     unsigned x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const unsigned*>(src + i * k16 * 2);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const unsigned pick = j ? 0x07060302u : 0x05040100u;
-      const int c = lds[raw + lay.off_idx + e + j], ch = c < kD ? c : kD;
+      const int c = lds[raw + a.off_idx + e + j], ch = c < kD ? c : kD;
       *reinterpret_cast<uint4*>(lds + keys + ch * kRowBytes + ((tg ^ twist(ch)) << 4)) =
           make_uint4(__builtin_amdgcn_perm(x[1], x[0], pick), __builtin_amdgcn_perm(x[3], x[2], pick),
                      __builtin_amdgcn_perm(x[5], x[4], pick), __builtin_amdgcn_perm(x[7], x[6], pick));
@@ -258,11 +258,10 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const CacheView&
 
 // The staged tile's values into `values` (a row per channel): threads 256 .. 511, a word of 16 tokens of one channel at a time.
 // Places of tokens that the tile does not have become 0 (their weights are 0, and 0 times what the LDS held may be NaN).
-__device__ __forceinline__ void unpack_values(unsigned char* lds, const CacheView& cv, int values, int n_tok) {
-  const Layout& lay = cv.lay;
+__device__ __forceinline__ void unpack_values(unsigned char* lds, const ChunkArgs& a, int values, int n_tok) {
   const int tid = threadIdx.x - 256, ch = tid & (kD - 1), first = __builtin_amdgcn_readfirstlane(tid >> 7);
-  const int per = cv.cfg.R >> 4, inv = 256 / per + 1;      // words of a record and channel; w / per = w inv >> 8 for w < 8
-  const int vg = ch / cv.cfg.Gv, row = values + ch * kRowBytes, tw = twist(ch);
+  const int per = a.R >> 4, inv = 256 / per + 1;      // words of a record and channel; w / per = w inv >> 8 for w < 8
+  const int vg = ch / a.Gv, row = values + ch * kRowBytes, tw = twist(ch);
 #pragma unroll 2
   for (int k = 0; k < 4; ++k) {
     const int w = first + 2 * k;
@@ -270,9 +269,9 @@ __device__ __forceinline__ void unpack_values(unsigned char* lds, const CacheVie
     int t0 = 16 * w, t1 = t0 + 8;
     if (t0 < n_tok) {
       const int rec = w * inv >> 8, in = w - rec * per;
-      const unsigned x = *reinterpret_cast<const unsigned*>(lds + kOffRaw + rec * lay.rec_bytes + lay.off_v + (in * kD + ch) * 4);
-      if (lay.v_interleave) {
-        t0 = rec * cv.cfg.R + 64 * (in >> 2) + 8 * (in & 3);
+      const unsigned x = *reinterpret_cast<const unsigned*>(lds + kOffRaw + rec * a.rec_bytes + a.off_v + (in * kD + ch) * 4);
+      if (a.interleave) {
+        t0 = rec * a.R + 64 * (in >> 2) + 8 * (in & 3);
         t1 = t0 + 32;
       }
       const unsigned char* s = lds + kOffScale + vg * kScaleRow * 2;
@@ -289,57 +288,30 @@ __device__ __forceinline__ void unpack_values(unsigned char* lds, const CacheVie
   }
 }
 
-template <int ROW_GROUPS, bool SPLIT>
-__global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(CacheView cv, ChunkArgs a, ChunkLaunch l) {
+template <int ROW_GROUPS, class Counts>
+__global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(ChunkArgs a, Counts counts) {
   __shared__ __align__(256) unsigned char lds[kLdsBytes];
   constexpr int kRows = 32 * ROW_GROUPS;
   constexpr int kShares = 8 / ROW_GROUPS;              // wavefronts that share 32 rows, each with its slices of every tile
-  constexpr int kSlices = 4 / kShares > 0 ? 4 / kShares : 1;
+  constexpr int kSlices = 4 / kShares;                 // of a tile
   constexpr int kStep = kSlices >= 2 ? 2 : 1;          // slices taken together
-  const mixkvq_config& cfg = cv.cfg;
-  const Layout& lay = cv.lay;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = wave % ROW_GROUPS, share = wave / ROW_GROUPS;
-  const bool bf16 = cfg.in_dtype != 0;
+  const bool bf16 = a.bf16 != 0;
+  const ChunkPlace at = chunk_place(a, counts, blockIdx.x);
+  const int g = a.g, Hkv = a.Hkv, b = at.b, j = at.j, p = at.p, n_rec = at.n_rec, n_fp16 = at.n_fp16;
+  const int n_rows = at.n_new * g, rt = gridDim.y - 1 - blockIdx.y;      // the last tiles of rows see most tokens: first
+  if (rt * kRows >= n_rows) return;
   __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);           // MODE.FP16_OVFL: a dequantized value past 65504 stays there
-
-  // ---- which unit: neighbouring units (they share keys) on one XCD ----
-  int unit;
-  {
-    const int n = l.n_units, x = blockIdx.x & 7, y = blockIdx.x >> 3, whole = n >> 3, more = n & 7;
-    unit = x * whole + (x < more ? x : more) + y;
-  }
-  int sb = 0, base = 0;
-  if (l.same_units) {
-    sb = unit / l.same_units;
-    base = sb * l.same_units;
-  } else {
-    int hi = l.n_seq;      // the last sequence whose first unit is not past this one
-    while (hi - sb > 1) {
-      const int mid = (sb + hi) >> 1;
-      if (l.first_unit[mid] <= unit) sb = mid;
-      else hi = mid;
-    }
-    base = l.first_unit[sb];
-  }
-  const int g = cv.g, Hkv = cfg.Hkv, b = l.b0 + sb;
-  const int n_new = l.n_new[sb], n_rec = l.n_rec[sb];
-  const int n_fp16 = (int)(l.rows_splits[sb] & 0xffffu), n_splits = (int)(l.rows_splits[sb] >> 16);
-  const int n_rows = n_new * g, row_tiles = (n_rows + kRows - 1) / kRows;
-  int in = unit - base;
-  const int rt = row_tiles - 1 - in % row_tiles;       // the longest (last) tiles of rows first
-  in /= row_tiles;
-  const int split = in % n_splits, j = in / n_splits;
-  const int p = b * Hkv + j;
 
   // ---- query rows of this wavefront ----
   const int row0 = rt * kRows + 32 * group;
   const bool active = row0 < n_rows;
   const int row = row0 + (lane & 31) < n_rows ? row0 + (lane & 31) : n_rows - 1;
-  const int token = row / g, head = j * g + row % g;
+  const int token = row / g, q_head = j * g + row % g;
   Rows st;
   if (active) {
-    const __half* q = a.q + (int64_t)b * a.qs.b + (int64_t)head * a.qs.h + (int64_t)token * a.qs.t + 8 * (lane >> 5);
+    const __half* q = a.q + (int64_t)b * a.qs.b + (int64_t)q_head * a.qs.h + (int64_t)token * a.qs.t + 8 * (lane >> 5);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       st.q[i] = __builtin_bit_cast(h8, as_f16x8(*reinterpret_cast<const uint4*>(q + 16 * i), bf16));
@@ -351,36 +323,36 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
   st.m = -INFINITY;
   st.l = 0.f;
   const float c = a.scale * 1.4426950408889634f;      // scores in log2 units
-  const int see_min = __builtin_amdgcn_readfirstlane(row0 / g) + 1;                   // chunk tokens seen by the first and the last row
+  const int see_min = row0 / g + 1;                   // chunk tokens seen by the first and the last row
   const int last_row = row0 + 31 < n_rows ? row0 + 31 : n_rows - 1;
-  const int see_max = __builtin_amdgcn_readfirstlane(last_row / g) + 1;
+  const int see_max = last_row / g + 1;
 
   // ---- this split's tiles: records, fp16 rows of the cache, the chunk as far as the tile's last row sees it ----
-  const int tile_rec = l.tile_rec;
+  const int tile_rec = a.tile_rec;
   const int tile_last = rt * kRows + kRows < n_rows ? rt * kRows + kRows - 1 : n_rows - 1;
   const int seen = tile_last / g + 1;
   const int nt_rec = (n_rec + tile_rec - 1) / tile_rec, nt_win = (n_fp16 + kChunkTile - 1) / kChunkTile;
   const int nt = nt_rec + nt_win + (seen + kChunkTile - 1) / kChunkTile;
-  const int t_first = (int)((long long)nt * split / n_splits), t_end = (int)((long long)nt * (split + 1) / n_splits);
+  const int t_first = (int)((long long)nt * at.split / at.n_splits), t_end = (int)((long long)nt * (at.split + 1) / at.n_splits);
 
   // ---- records ----
   const int r_end = t_end < nt_rec ? t_end : nt_rec;
   if (t_first < r_end) {
-    const int pieces = lay.rec_bytes >> 4;      // 16-byte pieces of a record
+    const int pieces = a.rec_bytes >> 4;      // 16-byte pieces of a record
     int pr[3], po[3], kind[3];                  // this thread's pieces of a tile: record, byte in it, plane
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       const int i = tid + kChunkThreads * k;
       pr[k] = i / pieces;
       po[k] = (i - pr[k] * pieces) * 16;
-      const int es = po[k] - lay.off_v_s, ez = po[k] - lay.off_v_z, plane = cfg.R * lay.NVG * 2;
+      const int es = po[k] - a.off_v_s, ez = po[k] - a.off_v_z, plane = a.R * a.NVG * 2;
       kind[k] = es >= 0 && es < plane ? 1 : ez >= 0 && ez < plane ? 2 : 0;
     }
-    const int32_t* table = cv.table ? cv.table + (size_t)b * cv.NB : nullptr;
-    const int nvg_bits = 31 - __builtin_clz(lay.NVG);
+    const int32_t* table = a.table ? a.table + (size_t)b * a.NB : nullptr;
+    const int nvg_bits = 31 - __builtin_clz(a.NVG);
     auto tile_count = [&](int t) { const int left = n_rec - t * tile_rec; return left < tile_rec ? left : tile_rec; };
     auto record = [&](int blk) {
-      return cv.blocks + (table ? (size_t)table[blk] * Hkv + j : (size_t)p * cv.NB + blk) * lay.rec_bytes;
+      return a.blocks + (table ? (size_t)table[blk] * Hkv + j : (size_t)p * a.NB + blk) * a.rec_bytes;
     };
     uint4 raw[3];
     auto fetch = [&](int t) {
@@ -395,25 +367,25 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
       for (int k = 0; k < 3; ++k) {
         if (pr[k] >= cnt) continue;
         if (kind[k] == 0) {
-          *reinterpret_cast<uint4*>(lds + kOffRaw + pr[k] * lay.rec_bytes + po[k]) = raw[k];
+          *reinterpret_cast<uint4*>(lds + kOffRaw + pr[k] * a.rec_bytes + po[k]) = raw[k];
         } else {      // value scales (zero-points): [token][group] there, [group][token] here
-          const int li = (po[k] - (kind[k] == 1 ? lay.off_v_s : lay.off_v_z)) >> 1;
-          unsigned short* to = reinterpret_cast<unsigned short*>(lds + kOffScale) + (kind[k] == 1 ? 0 : 8 * kScaleRow) + pr[k] * cfg.R;
+          const int li = (po[k] - (kind[k] == 1 ? a.off_v_s : a.off_v_z)) >> 1;
+          unsigned short* to = reinterpret_cast<unsigned short*>(lds + kOffScale) + (kind[k] == 1 ? 0 : 8 * kScaleRow) + pr[k] * a.R;
           const unsigned v[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int tok = (li + e) >> nvg_bits, vg = (li + e) & (lay.NVG - 1);
-            if (tok < cfg.R) to[vg * kScaleRow + tok] = (unsigned short)(v[e >> 1] >> (16 * (e & 1)));
+            const int tok = (li + e) >> nvg_bits, vg = (li + e) & (a.NVG - 1);
+            if (tok < a.R) to[vg * kScaleRow + tok] = (unsigned short)(v[e >> 1] >> (16 * (e & 1)));
           }
         }
       }
     };
     // Wavefront w lists record w's 2-bit channels: place -> row of the key tile (twisted), 128 for places without a channel.
-    const int ks = cfg.k4 + cfg.k16;
+    const int ks = a.k4 + a.k16;
     auto map_of = [&](int t) { return reinterpret_cast<unsigned short*>(lds + kOffMap) + (t & 1) * kChunkRecords * kD; };
     auto list_channels = [&](int t) {
       if (wave >= tile_count(t)) return;
-      const uint8_t* idx = record(t * tile_rec + wave) + lay.off_idx;
+      const uint8_t* idx = record(t * tile_rec + wave) + a.off_idx;
       unsigned long long low = ~0ull, high = ~0ull;      // channels 0 .. 63 and 64 .. 127 that are in no list
       const int e0 = lane < ks ? idx[lane] : 255, e1 = lane + 64 < ks ? idx[lane + 64] : 255;
       for (int e = 0; e < ks; ++e) {
@@ -434,8 +406,8 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
     stage(t_first);
     if (t_first + 1 < r_end) fetch(t_first + 1);
     __syncthreads();
-    if (wave < 4) unpack_keys(lds, cv, 0, map_of(t_first), tile_count(t_first) * cfg.R);
-    else unpack_values(lds, cv, kKeyBytes, tile_count(t_first) * cfg.R);
+    if (wave < 4) unpack_keys(lds, a, 0, map_of(t_first), tile_count(t_first) * a.R);
+    else unpack_values(lds, a, kKeyBytes, tile_count(t_first) * a.R);
     if (t_first + 1 < r_end) list_channels(t_first + 1);
     __syncthreads();
     for (int t = t_first; t < r_end; ++t) {
@@ -446,14 +418,14 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
       if (t + 2 < r_end) fetch(t + 2);
       // The wavefronts of a SIMD (w and w + 4) unpack the next tile at different times: one's vector instructions run beside
       // the other's matrix instructions.
-      if (next && wave < 4) unpack_keys(lds, cv, there, map_of(t + 1), tile_count(t + 1) * cfg.R);
+      if (next && wave < 4) unpack_keys(lds, a, there, map_of(t + 1), tile_count(t + 1) * a.R);
       if (active) {
-        const int n_tok = tile_count(t) * cfg.R;
+        const int n_tok = tile_count(t) * a.R;
 #pragma unroll 1
         for (int s = share * kSlices; s < (share + 1) * kSlices && s * 32 < n_tok; s += kStep)
           attend<kStep, true, true>(lds, here, here + kKeyBytes, s, st, c, (s + kStep) * 32 > n_tok, n_tok);
       }
-      if (next && wave >= 4) unpack_values(lds, cv, there + kKeyBytes, tile_count(t + 1) * cfg.R);
+      if (next && wave >= 4) unpack_values(lds, a, there + kKeyBytes, tile_count(t + 1) * a.R);
       if (t + 2 < r_end) list_channels(t + 2);
       __syncthreads();
     }
@@ -468,8 +440,8 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
     auto fetch = [&](int t) {
       const bool win = t < nt_rec + nt_win;
       const int first = (t - nt_rec - (win ? 0 : nt_win)) * kChunkTile, n = win ? n_fp16 : seen;
-      const __half* k = win ? cv.res_k + (size_t)p * cv.RW * kD : a.k + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
-      const __half* v = win ? cv.res_v + (size_t)p * cv.RW * kD : a.v + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
+      const __half* k = win ? a.res_k + (size_t)p * a.RW * kD : a.k + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
+      const __half* v = win ? a.res_v + (size_t)p * a.RW * kD : a.v + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
       const int64_t step = win ? kD : a.kvs.t;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -541,12 +513,12 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] += f * meet[at * kOutRow + chan + e];
     }
-    if constexpr (SPLIT) {
-      const size_t slot = (size_t)unit * kRows + r;
+    if (a.split) {
+      const size_t slot = ((size_t)blockIdx.x * gridDim.y + rt) * kRows + r;
       float* to = a.part + slot * kD + chan;
       *reinterpret_cast<f4*>(to) = f4{o[0], o[1], o[2], o[3]};
       *reinterpret_cast<f4*>(to + 4) = f4{o[4], o[5], o[6], o[7]};
-      if (chan == 0) *reinterpret_cast<float2*>(a.part + (size_t)l.n_units * kRows * kD + slot * 2) = make_float2(m, sum);
+      if (chan == 0) *reinterpret_cast<float2*>(a.part + (size_t)gridDim.x * gridDim.y * kRows * kD + slot * 2) = make_float2(m, sum);
     } else {
       const int t = rr / g, h = j * g + rr % g;
       const float inv = 1.f / sum;
@@ -557,24 +529,30 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Cache
         w[e] = bf16 ? (unsigned)f32_to_bf16_bits(x) | (unsigned)f32_to_bf16_bits(y) << 16 : as_u(__builtin_convertvector(f2{x, y}, h2));
       }
       *reinterpret_cast<uint4*>(a.out + (int64_t)b * a.os.b + (int64_t)h * a.os.h + (int64_t)t * a.os.t + chan) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (a.lse && chan == 0) a.lse[((size_t)b * cfg.Hq + h) * a.n_max + t] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+      if (a.lse && chan == 0) a.lse[((size_t)b * a.Hq + h) * a.n_max + t] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
   }
 }
 
-// The splits of a row meet: 16 threads to a row, per_pair workgroups to a (sequence, KV head) pair.
-__global__ void __launch_bounds__(256) chunk_merge_kernel(CacheView cv, ChunkArgs a, ChunkLaunch l, int rows, int per_pair) {
-  const int pair = blockIdx.x / per_pair, sb = pair / cv.cfg.Hkv, j = pair % cv.cfg.Hkv, g = cv.g;
-  const int n_rows = l.n_new[sb] * g, rr = blockIdx.x % per_pair * 16 + (threadIdx.x >> 4), chan = (threadIdx.x & 15) * 8;
-  if (rr >= n_rows) return;
-  const int n_splits = (int)(l.rows_splits[sb] >> 16), row_tiles = (n_rows + rows - 1) / rows, rt = rr / rows;
-  const int unit0 = (l.same_units ? sb * l.same_units : l.first_unit[sb]) + j * n_splits * row_tiles + row_tiles - 1 - rt;
-  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)l.n_units * rows * kD);
+// The splits of a row meet: 16 threads to a row; x: workgroups of 16 rows, y: pairs of the launch's sequences (in the order of
+// blockIdx.x of their first splits).
+template <class Counts>
+__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, Counts counts, int rows, int blocks, int per_pair) {
+  int pair = blockIdx.x / per_pair;
+  const int i = pair / a.Hkv, j = pair % a.Hkv;
+  ChunkPlace at;
+  if constexpr (std::is_same<Counts, NoChunkCounts>::value) at = chunk_place(a, counts, i * a.n_splits * a.Hkv + j);
+  else at = chunk_place(a, counts, counts.first[i] * a.Hkv + j);
+  const int g = a.g, n_rows = at.n_new * g, rr = blockIdx.x % per_pair * 16 + (threadIdx.x >> 4), chan = (threadIdx.x & 15) * 8;
+  if (rr >= n_rows || at.b != a.b0 + i) return;      // (a sequence without new tokens has no unit)
+  const size_t first = ((size_t)at.first_block * a.row_tiles + rr / rows) * rows + rr % rows, step = (size_t)a.Hkv * a.row_tiles * rows;
+  const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)blocks * rows * kD);
   float m = -INFINITY, sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < n_splits; ++s) m = fmaxf(m, ml[(size_t)(unit0 + s * row_tiles) * rows + rr % rows].x);
 #pragma unroll 4
-  for (int s = 0; s < n_splits; ++s) {
-    const size_t slot = (size_t)(unit0 + s * row_tiles) * rows + rr % rows;
+  for (int s = 0; s < at.n_splits; ++s) m = fmaxf(m, ml[first + s * step].x);
+#pragma unroll 4
+  for (int s = 0; s < at.n_splits; ++s) {
+    const size_t slot = first + s * step;
     const float2 x = ml[slot];
     const float f = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
     const f4 u = *reinterpret_cast<const f4*>(a.part + slot * kD + chan), v = *reinterpret_cast<const f4*>(a.part + slot * kD + chan + 4);
@@ -585,29 +563,31 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(CacheView cv, ChunkArg
       o[4 + e] += f * v[e];
     }
   }
-  const int b = l.b0 + sb, t = rr / g, h = j * g + rr % g;
+  const int t = rr / g, h = j * g + rr % g;
   const float inv = 1.f / sum;
   unsigned w[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float x = o[2 * e] * inv, y = o[2 * e + 1] * inv;
-    w[e] = cv.cfg.in_dtype ? (unsigned)f32_to_bf16_bits(x) | (unsigned)f32_to_bf16_bits(y) << 16 : as_u(__builtin_convertvector(f2{x, y}, h2));
+    w[e] = a.bf16 ? (unsigned)f32_to_bf16_bits(x) | (unsigned)f32_to_bf16_bits(y) << 16 : as_u(__builtin_convertvector(f2{x, y}, h2));
   }
-  *reinterpret_cast<uint4*>(a.out + (int64_t)b * a.os.b + (int64_t)h * a.os.h + (int64_t)t * a.os.t + chan) = make_uint4(w[0], w[1], w[2], w[3]);
-  if (a.lse && chan == 0) a.lse[((size_t)b * cv.cfg.Hq + h) * a.n_max + t] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  *reinterpret_cast<uint4*>(a.out + (int64_t)at.b * a.os.b + (int64_t)h * a.os.h + (int64_t)t * a.os.t + chan) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (a.lse && chan == 0) a.lse[((size_t)at.b * a.Hq + h) * a.n_max + t] = (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // |q| of the chunk joins the accumulator: exact integer sums, so that the order of the workgroups changes nothing.
-__global__ void __launch_bounds__(256) chunk_books_kernel(CacheView cv, ChunkArgs a, ChunkLaunch l, int per_pair) {
-  const int pair = blockIdx.x / per_pair, sb = pair / cv.cfg.Hkv, j = pair % cv.cfg.Hkv, g = cv.g, b = l.b0 + sb;
-  const int d = threadIdx.x & (kD - 1), n_rows = l.n_new[sb] * g, first = blockIdx.x % per_pair * 64;
-  const bool bf16 = cv.cfg.in_dtype != 0;
+template <class Counts>
+__global__ void __launch_bounds__(256) chunk_books_kernel(unsigned long long* qacc, unsigned long long* qcnt, ChunkArgs a, Counts counts, int per_pair) {
+  const int pair = blockIdx.x / per_pair, i = pair / a.Hkv, j = pair % a.Hkv, g = a.g, b = a.b0 + i;
+  int n_new = a.n_new;
+  if constexpr (!std::is_same<Counts, NoChunkCounts>::value) n_new = counts.n_new[i];
+  const int d = threadIdx.x & (kD - 1), n_rows = n_new * g, first = blockIdx.x % per_pair * 64;
   unsigned long long sum = 0;
   for (int r = first + (threadIdx.x >> 7); r < n_rows && r < first + 64; r += 2)
-    sum += fix24_abs(in_bits(a.q + (int64_t)b * a.qs.b + (int64_t)(j * g + r % g) * a.qs.h + (int64_t)(r / g) * a.qs.t + d, bf16));
-  const int p = b * cv.cfg.Hkv + j;
-  if (sum) atomicAdd(cv.qacc + (size_t)p * kD + d, sum);
-  if (first == 0 && threadIdx.x == 0 && n_rows) atomicAdd(cv.qcnt + p, (unsigned long long)n_rows);
+    sum += fix24_abs(in_bits(a.q + (int64_t)b * a.qs.b + (int64_t)(j * g + r % g) * a.qs.h + (int64_t)(r / g) * a.qs.t + d, a.bf16 != 0));
+  const int p = b * a.Hkv + j;
+  if (sum) atomicAdd(qacc + (size_t)p * kD + d, sum);
+  if (first == 0 && threadIdx.x == 0 && n_rows) atomicAdd(qcnt + p, (unsigned long long)n_rows);
 }
 
 int chunk_tile_records(const CacheView& v) {
@@ -617,49 +597,41 @@ int chunk_tile_records(const CacheView& v) {
   return n < kChunkRecords ? n : kChunkRecords;
 }
 
-template <int ROW_GROUPS>
-static void start_chunk(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s) {
-  if (split) chunk_attention_kernel<ROW_GROUPS, true><<<l.n_units, kChunkThreads, 0, s>>>(v, a, l);
-  else chunk_attention_kernel<ROW_GROUPS, false><<<l.n_units, kChunkThreads, 0, s>>>(v, a, l);
-}
-
-static int most_rows(const CacheView& v, const ChunkLaunch& l) {
-  int most = 0;
-  for (int i = 0; i < l.n_seq; ++i) most = l.n_new[i] > most ? l.n_new[i] : most;
-  return most * v.g;
-}
-
-hipError_t start_chunk_few_1(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s);
-hipError_t start_chunk_few_2(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s);
-hipError_t start_chunk_few_3(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool split, hipStream_t s);
-
-// Slices of 32 tokens inside one record and one key group; two to four steps of 32 channel places with nothing but 2-bit codes
-// and one with the rest, at most one step of fp16 places.
+// Slices of 32 tokens inside one record and one key group; four or five steps of channel places, at most one of fp16 places.
 bool chunk_few_fits(const CacheView& v) {
-  const int octets = v.lay.NLp / 8 + v.lay.W4;
-  return v.cfg.R % 32 == 0 && v.cfg.Gk % 32 == 0 && v.lay.NVG <= 4 && v.cfg.k16 <= 32 &&
-         (v.lay.NLp == 128 ? octets <= 20 : v.lay.NLp >= 96 && octets <= 16);
+  return v.cfg.R % 32 == 0 && v.cfg.Gk % 32 == 0 && v.lay.NVG <= 4 && v.cfg.k16 <= 32 && v.lay.W4 <= 4;
 }
 
-hipError_t launch_chunk(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, bool few, int rows, bool split, hipStream_t s) {
-  hipError_t e = hipSuccess;
-  if (few) {
-    e = rows == 16 ? start_chunk_few_1(v, a, l, split, s) : rows == 32 ? start_chunk_few_2(v, a, l, split, s) : start_chunk_few_3(v, a, l, split, s);
-  } else {
-    if (rows == 64) start_chunk<2>(v, a, l, split, s);
-    else if (rows == 128) start_chunk<4>(v, a, l, split, s);
-    else start_chunk<8>(v, a, l, split, s);
-    e = hipGetLastError();
-  }
-  if (e != hipSuccess || !split) return e;
-  const int per_pair = (most_rows(v, l) + 15) / 16;
-  chunk_merge_kernel<<<per_pair * l.n_seq * v.cfg.Hkv, 256, 0, s>>>(v, a, l, rows, per_pair);
+// 48 where the four steps hold everything and a token has one value group; the others have no registers for as many.
+int chunk_few_rows(const CacheView& v) { return v.cfg.k16 == 0 && chunk_few_steps(v.lay.NLp, v.lay.W4) == 4 && v.lay.NVG == 1 ? 48 : 32; }
+
+hipError_t start_chunk_few_1(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
+hipError_t start_chunk_few_2(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
+hipError_t start_chunk_few_3(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
+
+template <int ROW_GROUPS>
+static hipError_t start_tiles(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s) {
+  const dim3 grid(units * a.Hkv, a.row_tiles);
+  if (c) chunk_attention_kernel<ROW_GROUPS, ChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, *c);
+  else chunk_attention_kernel<ROW_GROUPS, NoChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, NoChunkCounts{});
   return hipGetLastError();
 }
 
-hipError_t launch_chunk_books(const CacheView& v, const ChunkArgs& a, const ChunkLaunch& l, hipStream_t s) {
-  const int per_pair = (most_rows(v, l) + 63) / 64;
-  chunk_books_kernel<<<per_pair * l.n_seq * v.cfg.Hkv, 256, 0, s>>>(v, a, l, per_pair);
+hipError_t launch_chunk(const ChunkArgs& a, const ChunkCounts* c, int units, int n_seq, bool few, int rows, hipStream_t s) {
+  hipError_t e;
+  if (few) e = rows == 16 ? start_chunk_few_1(a, c, units, s) : rows == 32 ? start_chunk_few_2(a, c, units, s) : start_chunk_few_3(a, c, units, s);
+  else e = rows == 64 ? start_tiles<2>(a, c, units, s) : rows == 128 ? start_tiles<4>(a, c, units, s) : start_tiles<8>(a, c, units, s);
+  if (e != hipSuccess || !a.split) return e;
+  const int per_pair = (a.row_tiles * rows + 15) / 16, blocks = units * a.Hkv * a.row_tiles;
+  if (c) chunk_merge_kernel<<<per_pair * n_seq * a.Hkv, 256, 0, s>>>(a, *c, rows, blocks, per_pair);
+  else chunk_merge_kernel<<<per_pair * n_seq * a.Hkv, 256, 0, s>>>(a, NoChunkCounts{}, rows, blocks, per_pair);
+  return hipGetLastError();
+}
+
+hipError_t launch_chunk_books(const CacheView& v, const ChunkArgs& a, const ChunkCounts* c, int n_seq, int n_most, hipStream_t s) {
+  const int per_pair = (n_most * a.g + 63) / 64;
+  if (c) chunk_books_kernel<<<per_pair * n_seq * a.Hkv, 256, 0, s>>>(v.qacc, v.qcnt, a, *c, per_pair);
+  else chunk_books_kernel<<<per_pair * n_seq * a.Hkv, 256, 0, s>>>(v.qacc, v.qcnt, a, NoChunkCounts{}, per_pair);
   return hipGetLastError();
 }
 

@@ -15,14 +15,16 @@ def kept(t: torch.Tensor) -> np.ndarray:
     return t.cpu().numpy().astype(np.float64)
 
 
-def chunk_reference(K0, V0, q, k, v, scale, out_half, key_size=None):
+def chunk_reference(K0, V0, q, k, v, scale, out_half, key_size=None, rounds=None):
     """One KV head: K0, V0 [T, D] cached (64 bits), q [g, n, D], k, v [n, D].  Returns out [g, n, D], lse [g, n] and how far the
     kernel's may be from them.
 
     The weights are those of scores off by at most E_t: keys rounded to binary16 (half a step each, or 2^-25 below its normal
     range) and binary32 sums of 128 products.  With sum_t w_t (v_t - o) = 0 that moves the output by at most
     sum_t w_t (e^E_t - 1) |v_t - o| e^max(E).  Weights and values are rounded to binary16 (half a step each; a weight below
-    2^-14 of the largest loses up to 2^-25), the sums over T tokens are binary32, the output is rounded once.
+    2^-14 of the largest loses up to 2^-25), the sums over T tokens are binary32, the output is rounded once.  Where a token has
+    one value group the kernel rounds p s instead of the value c s + z (Eq. 3): half a step of c s, which is the value less its
+    group's smallest (that one has code 0); rounds [T, D]: what half a step is relative to, |values| unless given.
     key_size [T, D]: what half a step of binary16 is relative to in the scores, |keys| unless given.
     """
     g, n, D = q.shape
@@ -46,10 +48,21 @@ def chunk_reference(K0, V0, q, k, v, scale, out_half, key_size=None):
     # sum_t grow_t |v_t - o|, channel by channel
     err = np.stack([np.einsum("gnt,gntd->gnd", grow[:, i:i + 1], np.abs(V[None, None] - o[:, i:i + 1, None])) for i in range(n)], 1)[:, :, 0] * up
     size = w @ np.abs(V)
-    err += up * size * (2 * HALF + (T + 2) * 2.0 ** -24) + np.abs(V).sum(0) * 2.0 ** -24
+    err += up * (size * HALF + (size if rounds is None else w @ rounds) * (HALF + (T + 2) * 2.0 ** -24)) + np.abs(V).sum(0) * 2.0 ** -24
     err += out_half * (np.abs(o) + err) + 2.0 ** -25
     lse_err = Emax[..., 0] + (T + 4) * 2.0 ** -24 + 2.0 ** -21 * (1 + np.abs(m + np.log(l))[..., 0])
     return o, (m + np.log(l))[..., 0], err, lse_err
+
+
+def value_rounds(oc, p, v):
+    """What the values' rounding is relative to, [T, D] over the cached tokens and the new ones."""
+    if oc.n_quant + oc.n_res + oc.n_sink == 0:
+        return np.abs(v)
+    V0 = oc.dequantized(p)[1]
+    size = np.abs(np.concatenate([V0, v]))
+    if oc.cfg.Gv == oc.cfg.D:
+        size[:V0.shape[0]] += V0 - V0.min(axis=1, keepdims=True)      # (binary32 sums of both parts: their sizes add)
+    return size
 
 
 def check_chunk(oc_of, g, Hkv, q, k, v, n_seq, out, lse, scale=None, name=""):
@@ -67,7 +80,8 @@ def check_chunk(oc_of, g, Hkv, q, k, v, n_seq, out, lse, scale=None, name=""):
         for j in range(Hkv):
             K0, V0 = oc.dequantized(p0 + j) if oc.n_quant + oc.n_res + oc.n_sink else (np.zeros((0, 128)),) * 2
             hs = slice(j * g, (j + 1) * g)
-            o, l, err, lerr = chunk_reference(K0, V0, qh[b, hs, :n], kh[b, j, :n], vh[b, j, :n], scale, out_half)
+            o, l, err, lerr = chunk_reference(K0, V0, qh[b, hs, :n], kh[b, j, :n], vh[b, j, :n], scale, out_half,
+                                              rounds=value_rounds(oc, p0 + j, vh[b, j, :n]))
             d = np.abs(got[b, hs, :n] - o)
             assert np.all(np.isfinite(got[b, hs, :n])), (name, b, j, "not finite")
             assert np.all(d <= err), (name, b, j, float((d / err).max()), float(d.max()))

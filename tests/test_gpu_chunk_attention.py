@@ -152,8 +152,10 @@ def test_one_new_token_agrees_with_the_decode_step(H):
             K0, V0 = oc_before[b * 2 + j]
             hs = slice(7 * j, 7 * j + 7)
             size = np.broadcast_to(np.ptp(np.concatenate([K0, kh[b, j]]), axis=0), (K0.shape[0] + 1, 128))
-            o, l, e1, l1 = H.chunk.chunk_reference(K0, V0, qh[b, hs], kh[b, j], vh[b, j], 1 / np.sqrt(128.0), 2.0 ** -11)
-            _, _, e2, l2 = H.chunk.chunk_reference(K0, V0, qh[b, hs], kh[b, j], vh[b, j], 1 / np.sqrt(128.0), 2.0 ** -11, key_size=size)
+            rounds = np.abs(np.concatenate([V0, vh[b, j]]))
+            rounds[:-1] += V0 - V0.min(axis=1, keepdims=True)
+            o, l, e1, l1 = H.chunk.chunk_reference(K0, V0, qh[b, hs], kh[b, j], vh[b, j], 1 / np.sqrt(128.0), 2.0 ** -11, rounds=rounds)
+            _, _, e2, l2 = H.chunk.chunk_reference(K0, V0, qh[b, hs], kh[b, j], vh[b, j], 1 / np.sqrt(128.0), 2.0 ** -11, key_size=size, rounds=rounds)
             assert np.all(np.abs(a[b, hs] - o[:, 0]) <= e1[:, 0]) and np.all(np.abs(a[b, hs] - r[b, hs]) <= e1[:, 0] + e2[:, 0])
             assert np.all(np.abs(al[b, hs] - l[:, 0]) <= l1[:, 0]) and np.all(np.abs(al[b, hs] - rl[b, hs]) <= l1[:, 0] + l2[:, 0])
 
