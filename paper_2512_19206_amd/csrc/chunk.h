@@ -27,7 +27,9 @@ struct ChunkArgs {
   int32_t n_rec, n_fp16, n_new, n_splits;      // of every sequence, unless the launch has ChunkCounts
   int32_t row_tiles, split;            // tiles of query rows (grid's y); is any sequence split?
   int32_t NB, RW, Hkv, Hq, g, bf16;
-  int32_t R, Gk, Gv, k4, k16, rec_bytes, tile_rec;
+  int32_t R, Gk, k4, k16, rec_bytes, tile_rec;
+  int32_t inv_r, inv_gk;               // x inv_r >> 16 is x / R for x <= 128, and so with Gk
+  int32_t nvg_bits;                    // NVG is two to this
   int32_t NLp, Wlo, W4, NVG, interleave;
   int32_t off_idx, off_kmax, off_klo_s, off_klo_z, off_k4_s, off_k4_z, off_klo, off_k4, off_k16, off_v, off_v_s, off_v_z;
 };
@@ -80,7 +82,7 @@ __device__ __forceinline__ ChunkPlace chunk_place(const ChunkArgs& a, const Chun
   return w;
 }
 
-// rows: query rows of a workgroup (tile kernel 64, 128 or 256; few rows 16, 32 or 48).  c == nullptr: equal counts.
+// rows: query rows of a workgroup (tile kernel 128 or 256; few rows 16, 32 or 48).  c == nullptr: equal counts.
 hipError_t launch_chunk(const ChunkArgs& a, const ChunkCounts* c, int units, int n_seq, bool few, int rows, hipStream_t s);
 hipError_t launch_chunk_books(const CacheView& v, const ChunkArgs& a, const ChunkCounts* c, int n_seq, int n_most, hipStream_t s);      // |q| of the chunk
 int chunk_tile_records(const CacheView& v);      // records of one tile

@@ -40,13 +40,20 @@ static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_s
   const int rows = most * c->v.g;
   pl.few = rows <= kFewRows && chunk_few_fits(c->v);
   if (pl.few) pl.rows = rows <= 16 ? 16 : rows <= 32 || chunk_few_rows(c->v) == 32 ? 32 : 48;
-  else pl.rows = rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-  // The splits' length that takes the least time: rounds of workgroups times what one does, its steps and a constant part, and
-  // more where the splits have to be merged.
-  int longest = 1;
+  else pl.rows = 256;
+  // The splits' length that takes the least time, counted in steps.  A unit costs its steps and a constant part.  Workgroups
+  // of one length run in rounds; of several (later rows of a chunk see more tokens, and the longest start first) they fill the
+  // compute units evenly until the shortest ones end.  Splits have to be merged, which costs a launch and their rows' traffic.
+  const int fixed = pl.few ? 3 : 2;
+  int longest = 1, shortest = 1 << 30;
+  bool equal = true;      // (the longest start first only among a sequence's own row tiles)
   for (int b = 0; b < cfg.B; ++b) {
-    const int n = n_new_of(n_seq, n_max, b), t = n ? chunk_steps(c, pl.few, b, n) : 0;
+    const int n = n_new_of(n_seq, n_max, b);
+    if (!n) continue;
+    const int t = chunk_steps(c, pl.few, b, n), t0 = chunk_steps(c, pl.few, b, 1);
+    equal = equal && (longest == 1 || t == longest);
     longest = t > longest ? t : longest;
+    shortest = t0 < shortest ? t0 : shortest;
   }
   double best = 0;
   pl.chain = longest;
@@ -54,11 +61,17 @@ static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_s
     const int chain = div_up(longest, s);
     if (s > 1 && chain == div_up(longest, s - 1)) continue;
     int64_t units = 0;
+    double steps = 0;
     for (int b = 0; b < cfg.B; ++b) {
       const int n = n_new_of(n_seq, n_max, b);
-      if (n) units += (int64_t)cfg.Hkv * div_up(n * c->v.g, pl.rows) * splits_of(chunk_steps(c, pl.few, b, n), chain);
+      if (!n) continue;
+      const int64_t tiles = (int64_t)cfg.Hkv * div_up(n * c->v.g, pl.rows);
+      units += tiles * splits_of(chunk_steps(c, pl.few, b, n), chain);
+      steps += (double)tiles * (chunk_steps(c, pl.few, b, n) + chunk_steps(c, pl.few, b, n < pl.rows / c->v.g ? n : pl.rows / c->v.g + 1)) / 2;
     }
-    const double t = (double)((units + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain + 3) + (s > 1 ? 4 : 0);
+    const double rounds = (double)((units + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain + fixed);
+    const double even = (steps + (double)fixed * units) / kChunkUnitsAtOnce + (equal && shortest < chain ? shortest : chain) + fixed;
+    const double t = (rounds < even ? rounds : even) + (s > 1 ? fixed + units * pl.rows / 32768.0 : 0);
     if (s == 1 || t < best) {
       best = t;
       pl.chain = chain;
@@ -197,7 +210,9 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
   a.bf16 = cfg.in_dtype != 0;
   a.R = cfg.R;
   a.Gk = cfg.Gk;
-  a.Gv = cfg.Gv;
+  a.inv_r = 65536 / cfg.R + 1;
+  a.inv_gk = 65536 / cfg.Gk + 1;
+  a.nvg_bits = 31 - __builtin_clz(lay.NVG);
   a.k4 = cfg.k4;
   a.k16 = cfg.k16;
   a.rec_bytes = lay.rec_bytes;

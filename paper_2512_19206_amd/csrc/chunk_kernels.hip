@@ -32,7 +32,8 @@ constexpr int kOffMap = kOffScale + 2 * 8 * kScaleRow * 2;       // [2][kChunkRe
 constexpr int kLdsBytes = kOffMap + 2 * kChunkRecords * kD * 2;
 static_assert(kLdsBytes <= 160 * 1024, "LDS of a compute unit");
 constexpr int kOutRow = kD + 4;                                  // floats of a row where the wavefronts' results meet
-static_assert(8 * 32 * kOutRow * 4 + 8 * 32 * 8 <= kLdsBytes, "results of eight wavefronts");
+constexpr int kRows = 256;                                        // query rows of a workgroup: 32 to a wavefront
+static_assert(kRows * kOutRow * 4 + kRows * 8 <= kLdsBytes, "the results");
 
 // A tile is 128 rows of 16 pieces of 16 bytes; piece c of row r lies at place c ^ twist(r), so that neither eight lanes with
 // neighbouring rows nor the transposing reads (four rows, two pieces) meet in a bank.
@@ -50,16 +51,24 @@ __device__ __forceinline__ unsigned as_u(h2 v) { return __builtin_bit_cast(unsig
 
 // Codes 2 i and 2 i + 1 of a word (BITS each, the even one in the low half-word) times s plus z.  A code is read as the last
 // bits of a half with a fixed exponent (2^e + code, exact), 2^e is taken off (exact), and one multiply-add rounds once.
+// The masks come in vector registers: an instruction takes one constant, and with the mask as another one it would be two.
 template <int BITS, int I>
-__device__ __forceinline__ unsigned dequant(unsigned w, h2 s, h2 z) {
-  constexpr int kShift = BITS * I;                       // of the code in its half-word; it has to stand in the ten mantissa bits
-  constexpr int kUp = kShift + BITS <= 10 ? kShift : kShift - (BITS == 2 ? 10 : 8);
-  constexpr unsigned kMask = ((1u << BITS) - 1u) << kUp, kMagic = (unsigned)(15 + 10 - kUp) << 10;
+struct CodeAt {
+  static constexpr int kShift = BITS * I;                       // of the code in its half-word; it has to stand in the ten mantissa bits
+  static constexpr int kUp = kShift + BITS <= 10 ? kShift : kShift - (BITS == 2 ? 10 : 8);
   static_assert(kUp >= 0 && kUp + BITS <= 10, "inside the mantissa");
-  const unsigned x = kShift == kUp ? w : w >> (kShift - kUp);
-  const unsigned y = (x & (kMask * 0x10001u)) | (kMagic * 0x10001u);
-  const _Float16 off = (_Float16)(float)(1 << (10 - kUp));
-  return as_u((as_h2(y) - h2{off, off}) * s + z);
+  static constexpr unsigned kMask = (((1u << BITS) - 1u) << kUp) * 0x10001u, kMagic = ((unsigned)(25 - kUp) << 10) * 0x10001u;
+};
+template <int BITS, int I>
+__device__ __forceinline__ unsigned dequant(unsigned w, const unsigned (&mask)[5], h2 s, h2 z) {
+  typedef CodeAt<BITS, I> C;
+  const unsigned x = C::kShift == C::kUp ? w : w >> (C::kShift - C::kUp);
+  const _Float16 off = (_Float16)(float)(1 << (10 - C::kUp));
+  return as_u((as_h2((x & mask[C::kUp / BITS]) | C::kMagic) - h2{off, off}) * s + z);
+}
+__device__ __forceinline__ unsigned in_vgpr(unsigned x) {
+  asm("" : "+v"(x));
+  return x;
 }
 
 // State of one wavefront: 32 query rows, one to a lane and its partner 32 lanes away.
@@ -69,123 +78,210 @@ struct Rows {
   float m, l;         // reference of the exponents (log2 units) and this lane's share of the sum of the weights
 };
 
-// The largest score may run ahead of the reference by this much (in log2) before the sums are brought to a new reference:
-// weights stay below 2^8, well inside binary16, and most tiles change nothing.
-constexpr float kHeadroom = 8.f;
+// The kernel's arguments, read anew from where the launch put them (ChunkArgs is a kernel's first argument): what is read through this
+// is not kept in scalar registers across the loop, which runs out of them.
+typedef __attribute__((address_space(4))) const ChunkArgs ArgsIn;
+__device__ __forceinline__ ArgsIn& args_here() {
+  ArgsIn* x = (ArgsIn*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(x));
+  return *x;
+}
 
-// One pass over NS slices of 32 tokens of a tile.  BY_CHANNEL: the key tile has a row per channel (records), else a row per
-// token, and the value tile the other way round.  limit: tokens of the tile this lane's row may see; only where `masked`.
-template <int NS, bool BY_CHANNEL_K, bool BY_CHANNEL_V>
-__device__ __forceinline__ void attend(unsigned char* lds, int keys, int values, int slice, Rows& st, float c, bool masked, int limit) {
-  const int lane = threadIdx.x & 63, half = lane >> 5, i16 = lane & 15, grp = lane >> 4;
-  f16v s[NS];
+// The thread's number, found anew: what is made of it is not kept in registers from one tile to the next.
+__device__ __forceinline__ int tid_here() {
+  int x = threadIdx.x;
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The largest score may run ahead of the reference by this much (in log2) before the sums are brought to a new reference:
+// weights stay below 2^13, well inside binary16, and most tiles change nothing.
+constexpr float kHeadroom = 13.f;
+constexpr float kNoToken = -1e30f;      // reference of a row that has seen no token
+
+// Where a lane reads its operands: addresses that stand for a whole tile (the rest is the instructions' constant offset).  BY_CHANNEL: the
+// tiles have a row per channel (records), else a row per token.
+// Row 8 a + 4 h + i of a slice of 32 scores stands for token 16 (a / 2) + 8 h + 4 (a % 2) + i: a lane then holds runs of eight
+// neighbouring tokens, which is what the second product takes.
+template <bool BY_CHANNEL>
+struct Operands {
+  int k[8], v[8];
+  __device__ __forceinline__ Operands() {
+    const int lane = threadIdx.x & 63, half = lane >> 5, i16 = lane & 15, grp = lane >> 4, m = lane & 31;
+    const int row = 8 * (grp >> 1) + (i16 >> 2);      // of a transposing read, and four rows on
+    if constexpr (BY_CHANNEL) {
+      const int piece = 2 * (grp & 1) + (i16 & 1), sub = ((i16 >> 1) & 1) * 8;
 #pragma unroll
-  for (int n = 0; n < NS; ++n) {
+      for (int i = 0; i < 8; ++i) {                   // slice i / 2
+        k[i] = (row + 4 * (i & 1)) * kRowBytes + sub + ((piece ^ twist(row + 4 * (i & 1)) ^ (i >> 1) << 2) << 4);
+        v[i] = kKeyBytes + m * kRowBytes + ((half ^ twist(m) ^ i << 1) << 4);
+      }
+    } else {
+      const int token = 16 * (m >> 4) + 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3);
+      const int piece = 2 * (grp & 1) + ((i16 >> 1) & 1), sub = (i16 & 1) * 8;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
-  }
-  // Row 8 a + 4 h + i of a slice of scores stands for token 16 (a / 2) + 8 h + 4 (a % 2) + i: a lane then holds runs of eight
-  // neighbouring tokens, which is what the second product takes.
-  if constexpr (BY_CHANNEL_K) {
-    const int row = 8 * (grp >> 1) + (i16 >> 2), piece = 2 * (grp & 1) + (i16 & 1), sub = ((i16 >> 1) & 1) * 8;
-    const int a0 = keys + row * kRowBytes + sub, x0 = (piece ^ twist(row)) << 4, x1 = (piece ^ twist(row + 4)) << 4;
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      const int at0 = a0 + (x0 ^ ((slice + n) << 6)), at1 = a0 + 4 * kRowBytes + (x1 ^ ((slice + n) << 6));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const h8 k = join(lds_column(lds, at0 + i * 16 * kRowBytes), lds_column(lds, at1 + i * 16 * kRowBytes));
-        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, st.q[i], s[n], 0, 0, 0);
+      for (int i = 0; i < 8; ++i) {                   // channels 16 i .. of the keys, 32 (i / 2) .. of the values
+        k[i] = token * kRowBytes + ((half ^ twist(token) ^ i << 1) << 4);
+        v[i] = kKeyBytes + (row + 4 * (i & 1)) * kRowBytes + sub + ((piece ^ twist(row + 4 * (i & 1)) ^ (i >> 1) << 2) << 4);
       }
     }
-  } else {
-    const int m = lane & 31, token = 16 * (m >> 4) + 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3);
-    const int a0 = keys + token * kRowBytes, x = (half ^ twist(token)) << 4;
-#pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const h8 k = lds_h8(lds, a0 + (slice + n) * 32 * kRowBytes + (x ^ (i << 5)));
-        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, st.q[i], s[n], 0, 0, 0);
-      }
+    move(k, 0);
+    move(v, 0);
   }
-  if (masked) {
+  // To the other of the two tiles in LDS.
+  static __device__ __forceinline__ void move(int (&x)[8], int by) {
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if ((slice + n) * 32 + 16 * (r >> 3) + 8 * half + (r & 7) >= limit) s[n][r] = -INFINITY;
+    for (int i = 0; i < 8; ++i) {
+      x[i] += by;
+      asm volatile("" : "+v"(x[i]));
+    }
   }
-  float mx = s[0][0];
-#pragma unroll
-  for (int n = 0; n < NS; ++n)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[n][r]);
-  {
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
+  // Channels 16 i .. of a slice's keys.
+  __device__ __forceinline__ h8 key(unsigned char* lds, int slice, int i) const {
+    if constexpr (BY_CHANNEL)
+      return join(lds_column(lds, k[2 * slice] + i * 16 * kRowBytes), lds_column(lds, k[2 * slice + 1] + i * 16 * kRowBytes));
+    else
+      return lds_h8(lds, k[i] + slice * 32 * kRowBytes);
   }
+  // Channels 32 c .. at tokens 16 t .. of a slice's values.
+  __device__ __forceinline__ h8 value(unsigned char* lds, int slice, int t, int c) const {
+    if constexpr (BY_CHANNEL)
+      return lds_h8(lds, v[2 * slice + t] + c * 32 * kRowBytes);
+    else
+      return join(lds_column(lds, v[2 * c] + (slice * 32 + t * 16) * kRowBytes), lds_column(lds, v[2 * c + 1] + (slice * 32 + t * 16) * kRowBytes));
+  }
+};
+
+// Tokens of the tile from `limit` on do not count for this lane's row.
+__device__ __forceinline__ void hide(int slice, int limit, f16v& s) {
+  const int left = limit - slice * 32 - 8 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (16 * (r >> 3) + (r & 7) >= left) s[r] = -INFINITY;
+}
+
+__device__ __forceinline__ float largest(const f16v& s) {
+  float mx = s[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+  return mx;
+}
+
+// Brings the sums and the weights that are still to be used to a new reference if a score (mx: this lane's largest) has run too far
+// ahead; only then do the two lanes of a row agree on it.  References are whole numbers: the weights' factor is a power of two.
+__device__ __forceinline__ void follow(float mx, Rows& st, h8 (&p)[2]) {
   if (__any(mx > st.m + kHeadroom)) {
-    const float m = fmaxf(st.m, mx);
-    const float f = m == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    const float m = ceilf(fmaxf(st.m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])))), f = __builtin_amdgcn_exp2f(st.m - m);
     st.m = m;
     st.l *= f;
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[b][r] *= f;
+    const _Float16 f16 = (_Float16)f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] *= h8{f16, f16, f16, f16, f16, f16, f16, f16};
   }
-  const float ref = st.m == -INFINITY ? 0.f : st.m;      // (a row that has seen no token yet)
-  h8 p[NS][2];
+}
+
+// What a wavefront carries from step to step.
+template <bool BY_CHANNEL>
+struct Pipe {
+  Operands<BY_CHANNEL> at;
+  h8 k[4], v[4];      // the next operands of the two products: a ring, each refilled four matrix instructions ahead
+};
+
+// One step of a wavefront, on three slices at once: the scores of slice SLICE + 1 are formed (`next`), those of slice SLICE (`cur`, hidden
+// and followed) become weights (`p`), and the values of the slice before are added with its weights (`before`).  Nothing of
+// this depends on anything else of it, and the order is fixed piece by piece: every matrix instruction finds its operands in
+// registers and has a sixteenth of the vector instructions behind it, so that neither the LDS nor the exponentials are waited for.
+// Out: the next scores, hidden and followed.
+template <int SLICE, bool BY_CHANNEL>
+__device__ __forceinline__ void step(unsigned char* lds, Pipe<BY_CHANNEL>& in, int move, f16v& cur, f16v& next, const h8 (&before)[2], h8 (&p)[2],
+                                     bool masked, int limit, float c, Rows& st) {
+  float sum = 0.f, mx = 0.f;
 #pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    float sum = 0.f;
+  for (int r = 0; r < 16; ++r) next[r] = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], c, -ref)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + 1], c, -ref));
-      sum += e0 + e1;
-      const h2 e = __builtin_convertvector(f2{e0, e1}, h2);      // nearest: a truncated weight would pull every output to zero
-      p[n][r >> 3][r & 7] = e[0];
-      p[n][r >> 3][(r & 7) + 1] = e[1];
+  for (int s = 0, e = 0; s < 16; ++s) {
+    if (s < 12 && s % 3 != 2) {
+      const int i = s - s / 3;
+      next = __builtin_amdgcn_mfma_f32_32x32x16_f16(in.k[i & 3], st.q[i], next, 0, 0, 0);
+      if (SLICE == 2 && i == 4) in.at.move(in.at.k, move);      // the keys that follow are the next tile's
+      in.k[i & 3] = in.at.key(lds, (SLICE + (i < 4 ? 1 : 2)) & 3, (i + 4) & 7);
+    } else {
+      const int i = s < 12 ? s / 3 : s - 8;
+      st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(in.v[i & 3], before[i >> 2], st.o[i & 3], 0, 0, 0);
+      if (SLICE == 0 && i == 4) in.at.move(in.at.v, move);      // the values that follow are this tile's
+      in.v[i & 3] = in.at.value(lds, (SLICE + (i < 4 ? 3 : 0)) & 3, i < 4, i & 3);
     }
-    st.l += sum;
+    if (s * 2 >= e * 3 && e < 8) {
+      const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[2 * e], c, -st.m)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[2 * e + 1], c, -st.m));
+      const h2 w = __builtin_convertvector(f2{e0, e1}, h2);      // nearest: a truncated weight would pull every output to zero
+      sum = __builtin_amdgcn_fdot2(w, h2{(_Float16)1.f, (_Float16)1.f}, sum, false);
+      asm volatile("" : "+v"(sum));
+      p[e >> 2][2 * (e & 3)] = w[0];
+      p[e >> 2][2 * (e & 3) + 1] = w[1];
+      ++e;
+    }
+    if (s == 14) mx = largest(next);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  if constexpr (BY_CHANNEL_V) {
-    const int m = lane & 31, a0 = values + m * kRowBytes, x = (half ^ twist(m)) << 4;
+  st.l += sum;
+  if (masked) {
+    asm volatile("");      // (a branch, and not 16 selections in every step)
+    hide((SLICE + 1) & 3, limit, next);
+    mx = largest(next);
+  }
+  follow(mx * c, st, p);
+}
+
+// What the first step takes: the first slice's scores, no weights, operands in the rings.  Rows see `limit` tokens of the tile, all of
+// them `all`.
+template <bool BY_CHANNEL>
+__device__ __forceinline__ void begin(unsigned char* lds, Pipe<BY_CHANNEL>& in, int all, int limit, float c, f16v& s, h8 (&p)[2], Rows& st) {
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
+  for (int i = 0; i < 4; ++i) in.k[i] = in.at.key(lds, 0, i);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int at = a0 + (x ^ ((slice + n) << 6) ^ (t << 5));
+  for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-          st.o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_h8(lds, at + b * 32 * kRowBytes), p[n][t], st.o[b], 0, 0, 0);
-      }
-  } else {
-    const int row = 8 * (grp >> 1) + (i16 >> 2), piece = 2 * (grp & 1) + ((i16 >> 1) & 1), sub = (i16 & 1) * 8;
-    const int a0 = values + row * kRowBytes + sub, x0 = (piece ^ twist(row)) << 4, x1 = (piece ^ twist(row + 4)) << 4;
+  for (int i = 0; i < 8; ++i) {
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(in.k[i & 3], st.q[i], s, 0, 0, 0);
+    in.k[i & 3] = in.at.key(lds, i < 4 ? 0 : 1, (i + 4) & 7);
+  }
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
+  for (int i = 0; i < 2; ++i) p[i] = h8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int at = a0 + ((slice + n) * 32 + t * 16) * kRowBytes;
+  for (int i = 0; i < 4; ++i) in.v[i] = in.at.value(lds, 3, 0, i);      // (taken times 0)
+  if (32 > all) {
+    asm volatile("");
+    hide(0, limit, s);
+  }
+  follow(largest(s) * c, st, p);
+}
+
+// The last slice's values.
+template <bool BY_CHANNEL>
+__device__ __forceinline__ void finish(unsigned char* lds, Pipe<BY_CHANNEL>& in, const h8 (&p)[2], Rows& st) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const h8 v = join(lds_column(lds, at + (x0 ^ (b << 6))), lds_column(lds, at + 4 * kRowBytes + (x1 ^ (b << 6))));
-          st.o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[n][t], st.o[b], 0, 0, 0);
-        }
-      }
+  for (int i = 0; i < 8; ++i) {
+    st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(in.v[i & 3], p[i >> 2], st.o[i & 3], 0, 0, 0);
+    if (i < 4) in.v[i] = in.at.value(lds, 3, 1, i);
   }
 }
 
 // Dequantizes the staged tile's keys into `keys` (a row per channel).  Threads 0 .. 255; threads 256 .. 511 do the values.
-__device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs& a, int keys, const unsigned short* map, int n_tok) {
-  const int Rr = a.R, tid = threadIdx.x;
+__device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, const unsigned short* map, int n_tok) {
+  ArgsIn& a = args_here();
+  const int Rr = a.R, inv_r = a.inv_r, inv_gk = a.inv_gk, tid = tid_here();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const unsigned two[5] = {in_vgpr(CodeAt<2, 0>::kMask), in_vgpr(CodeAt<2, 1>::kMask), in_vgpr(CodeAt<2, 2>::kMask), in_vgpr(CodeAt<2, 3>::kMask), in_vgpr(CodeAt<2, 4>::kMask)};
+  const unsigned wide[5] = {in_vgpr(CodeAt<4, 0>::kMask), in_vgpr(CodeAt<4, 1>::kMask), 0, 0, 0};
   {  // 2-bit channels: eight tokens of the eight even or odd channels of a word
     const int odd = wave & 1, tg = (wave >> 1) * 8 + (lane & 7), w = lane >> 3, t = tg * 8;
     if (w < a.Wlo && t < n_tok) {
-      const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
+      const int rec = t * inv_r >> 16, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
       const int words = raw + a.off_klo + (tin * a.Wlo + w) * 4;
       const unsigned pick = odd ? 0x07060302u : 0x05040100u, twice = odd ? 0x03020302u : 0x01000100u;
       unsigned x[4];
@@ -193,7 +289,7 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs&
       for (int i = 0; i < 4; ++i)
         x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * a.Wlo * 4),
                                      *reinterpret_cast<const unsigned*>(lds + words + 2 * i * a.Wlo * 4), pick);
-      const int sc = raw + a.off_klo_s + ((tin / a.Gk) * a.NLp + 16 * w) * 2, zc = sc + a.off_klo_z - a.off_klo_s;
+      const int sc = raw + a.off_klo_s + ((tin * inv_gk >> 16) * a.NLp + 16 * w) * 2, zc = sc + a.off_klo_z - a.off_klo_s;
       const unsigned* s = reinterpret_cast<const unsigned*>(lds + sc);
       const unsigned* z = reinterpret_cast<const unsigned*>(lds + zc);
       const unsigned* at = reinterpret_cast<const unsigned*>(map + rec * kD + 16 * w);
@@ -202,8 +298,8 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs&
   {                                                                                                                        \
     const h2 s2 = as_h2(__builtin_amdgcn_perm(s[I], s[I], twice)), z2 = as_h2(__builtin_amdgcn_perm(z[I], z[I], twice));   \
     const int to = keys + (((at[I] >> (16 * odd)) & 0xffffu) ^ col);                                                       \
-    *reinterpret_cast<uint4*>(lds + to) = make_uint4(dequant<2, I>(x[0], s2, z2), dequant<2, I>(x[1], s2, z2),             \
-                                                     dequant<2, I>(x[2], s2, z2), dequant<2, I>(x[3], s2, z2));            \
+    *reinterpret_cast<uint4*>(lds + to) = make_uint4(dequant<2, I>(x[0], two, s2, z2), dequant<2, I>(x[1], two, s2, z2),             \
+                                                     dequant<2, I>(x[2], two, s2, z2), dequant<2, I>(x[3], two, s2, z2));            \
   }
       MIXKVQ_CHANNEL(0) MIXKVQ_CHANNEL(1) MIXKVQ_CHANNEL(2) MIXKVQ_CHANNEL(3)
       MIXKVQ_CHANNEL(4) MIXKVQ_CHANNEL(5) MIXKVQ_CHANNEL(6) MIXKVQ_CHANNEL(7)
@@ -215,7 +311,7 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs&
   for (int u = tid; u < a.W4 * 32; u += 256) {      // four bits: eight tokens of the four even or odd channels of a word
     const int odd = u & 1, tg = (u >> 1) & 15, w = u >> 5, t = tg * 8;
     if (t >= n_tok) continue;
-    const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
+    const int rec = t * inv_r >> 16, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
     const int words = raw + a.off_k4 + (tin * a.W4 + w) * 4;
     const unsigned pick = odd ? 0x07060302u : 0x05040100u, twice = odd ? 0x03020302u : 0x01000100u;
     unsigned x[4];
@@ -223,16 +319,16 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs&
     for (int i = 0; i < 4; ++i)
       x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * a.W4 * 4),
                                    *reinterpret_cast<const unsigned*>(lds + words + 2 * i * a.W4 * 4), pick);
-    const unsigned* s = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_s + ((tin / a.Gk) * k4 + 8 * w) * 2);
-    const unsigned* z = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_z + ((tin / a.Gk) * k4 + 8 * w) * 2);
+    const unsigned* s = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_s + ((tin * inv_gk >> 16) * k4 + 8 * w) * 2);
+    const unsigned* z = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_z + ((tin * inv_gk >> 16) * k4 + 8 * w) * 2);
     const unsigned char* list = lds + raw + a.off_idx + k16 + 8 * w + odd;
 #define MIXKVQ_CHANNEL(I)                                                                                                  \
   {                                                                                                                        \
     const h2 s2 = as_h2(__builtin_amdgcn_perm(s[I], s[I], twice)), z2 = as_h2(__builtin_amdgcn_perm(z[I], z[I], twice));   \
     const int ch = list[2 * I] < kD ? list[2 * I] : kD;                                                                    \
     const int to = keys + ch * kRowBytes + ((tg ^ twist(ch)) << 4);                                                        \
-    *reinterpret_cast<uint4*>(lds + to) = make_uint4(dequant<4, I>(x[0], s2, z2), dequant<4, I>(x[1], s2, z2),             \
-                                                     dequant<4, I>(x[2], s2, z2), dequant<4, I>(x[3], s2, z2));            \
+    *reinterpret_cast<uint4*>(lds + to) = make_uint4(dequant<4, I>(x[0], wide, s2, z2), dequant<4, I>(x[1], wide, s2, z2),             \
+                                                     dequant<4, I>(x[2], wide, s2, z2), dequant<4, I>(x[3], wide, s2, z2));            \
   }
     MIXKVQ_CHANNEL(0) MIXKVQ_CHANNEL(1) MIXKVQ_CHANNEL(2) MIXKVQ_CHANNEL(3)
 #undef MIXKVQ_CHANNEL
@@ -240,7 +336,7 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs&
   for (int u = tid; u < k16 * 8; u += 256) {      // fp16: eight tokens of two neighbouring entries
     const int tg = u & 15, e = (u >> 4) * 2, t = tg * 8;
     if (t >= n_tok) continue;
-    const int rec = t / Rr, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
+    const int rec = t * inv_r >> 16, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
     const unsigned char* src = lds + raw + a.off_k16 + (tin * k16 + e) * 2;
     unsigned x[8];
 #pragma unroll
@@ -258,17 +354,19 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, const ChunkArgs&
 
 // The staged tile's values into `values` (a row per channel): threads 256 .. 511, a word of 16 tokens of one channel at a time.
 // Places of tokens that the tile does not have become 0 (their weights are 0, and 0 times what the LDS held may be NaN).
-__device__ __forceinline__ void unpack_values(unsigned char* lds, const ChunkArgs& a, int values, int n_tok) {
-  const int tid = threadIdx.x - 256, ch = tid & (kD - 1), first = __builtin_amdgcn_readfirstlane(tid >> 7);
-  const int per = a.R >> 4, inv = 256 / per + 1;      // words of a record and channel; w / per = w inv >> 8 for w < 8
-  const int vg = ch / a.Gv, row = values + ch * kRowBytes, tw = twist(ch);
+__device__ __forceinline__ void unpack_values(unsigned char* lds, int values, int n_tok) {
+  ArgsIn& a = args_here();
+  const int tid = tid_here() - 256, ch = tid & (kD - 1), first = __builtin_amdgcn_readfirstlane(tid >> 7);
+  const unsigned two[5] = {in_vgpr(CodeAt<2, 0>::kMask), in_vgpr(CodeAt<2, 1>::kMask), in_vgpr(CodeAt<2, 2>::kMask), in_vgpr(CodeAt<2, 3>::kMask), in_vgpr(CodeAt<2, 4>::kMask)};
+  const int per = a.R >> 4;      // words of a record and channel
+  const int vg = ch >> (7 - a.nvg_bits), row = values + ch * kRowBytes, tw = twist(ch);
 #pragma unroll 2
   for (int k = 0; k < 4; ++k) {
     const int w = first + 2 * k;
     uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
     int t0 = 16 * w, t1 = t0 + 8;
     if (t0 < n_tok) {
-      const int rec = w * inv >> 8, in = w - rec * per;
+      const int rec = 16 * w * a.inv_r >> 16, in = w - rec * per;
       const unsigned x = *reinterpret_cast<const unsigned*>(lds + kOffRaw + rec * a.rec_bytes + a.off_v + (in * kD + ch) * 4);
       if (a.interleave) {
         t0 = rec * a.R + 64 * (in >> 2) + 8 * (in & 3);
@@ -278,25 +376,20 @@ __device__ __forceinline__ void unpack_values(unsigned char* lds, const ChunkArg
       const unsigned char* z = s + 8 * kScaleRow * 2;
       const uint4 s0 = *reinterpret_cast<const uint4*>(s + t0 * 2), z0 = *reinterpret_cast<const uint4*>(z + t0 * 2);
       const uint4 s1 = *reinterpret_cast<const uint4*>(s + t1 * 2), z1 = *reinterpret_cast<const uint4*>(z + t1 * 2);
-      lo = make_uint4(dequant<2, 0>(x, as_h2(s0.x), as_h2(z0.x)), dequant<2, 1>(x, as_h2(s0.y), as_h2(z0.y)),
-                      dequant<2, 2>(x, as_h2(s0.z), as_h2(z0.z)), dequant<2, 3>(x, as_h2(s0.w), as_h2(z0.w)));
-      hi = make_uint4(dequant<2, 4>(x, as_h2(s1.x), as_h2(z1.x)), dequant<2, 5>(x, as_h2(s1.y), as_h2(z1.y)),
-                      dequant<2, 6>(x, as_h2(s1.z), as_h2(z1.z)), dequant<2, 7>(x, as_h2(s1.w), as_h2(z1.w)));
+      lo = make_uint4(dequant<2, 0>(x, two, as_h2(s0.x), as_h2(z0.x)), dequant<2, 1>(x, two, as_h2(s0.y), as_h2(z0.y)),
+                      dequant<2, 2>(x, two, as_h2(s0.z), as_h2(z0.z)), dequant<2, 3>(x, two, as_h2(s0.w), as_h2(z0.w)));
+      hi = make_uint4(dequant<2, 4>(x, two, as_h2(s1.x), as_h2(z1.x)), dequant<2, 5>(x, two, as_h2(s1.y), as_h2(z1.y)),
+                      dequant<2, 6>(x, two, as_h2(s1.z), as_h2(z1.z)), dequant<2, 7>(x, two, as_h2(s1.w), as_h2(z1.w)));
     }
     *reinterpret_cast<uint4*>(lds + row + (((t0 >> 3) ^ tw) << 4)) = lo;
     *reinterpret_cast<uint4*>(lds + row + (((t1 >> 3) ^ tw) << 4)) = hi;
   }
 }
 
-template <int ROW_GROUPS, class Counts>
+template <class Counts>
 __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(ChunkArgs a, Counts counts) {
   __shared__ __align__(256) unsigned char lds[kLdsBytes];
-  constexpr int kRows = 32 * ROW_GROUPS;
-  constexpr int kShares = 8 / ROW_GROUPS;              // wavefronts that share 32 rows, each with its slices of every tile
-  constexpr int kSlices = 4 / kShares;                 // of a tile
-  constexpr int kStep = kSlices >= 2 ? 2 : 1;          // slices taken together
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int group = wave % ROW_GROUPS, share = wave / ROW_GROUPS;
   const bool bf16 = a.bf16 != 0;
   const ChunkPlace at = chunk_place(a, counts, blockIdx.x);
   const int g = a.g, Hkv = a.Hkv, b = at.b, j = at.j, p = at.p, n_rec = at.n_rec, n_fp16 = at.n_fp16;
@@ -305,7 +398,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
   __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);           // MODE.FP16_OVFL: a dequantized value past 65504 stays there
 
   // ---- query rows of this wavefront ----
-  const int row0 = rt * kRows + 32 * group;
+  const int row0 = rt * kRows + 32 * wave;
   const bool active = row0 < n_rows;
   const int row = row0 + (lane & 31) < n_rows ? row0 + (lane & 31) : n_rows - 1;
   const int token = row / g, q_head = j * g + row % g;
@@ -320,12 +413,12 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.o[c][r] = 0.f;
-  st.m = -INFINITY;
+  st.m = kNoToken;
   st.l = 0.f;
+  f16v sc[2];                                          // scores of this slice and of the next one, in turn
+  h8 pw[2][2];                                         // weights of this slice and of the one before, in turn
   const float c = a.scale * 1.4426950408889634f;      // scores in log2 units
-  const int see_min = row0 / g + 1;                   // chunk tokens seen by the first and the last row
-  const int last_row = row0 + 31 < n_rows ? row0 + 31 : n_rows - 1;
-  const int see_max = last_row / g + 1;
+  const int see_min = row0 / g + 1;                   // chunk tokens seen by the first row
 
   // ---- this split's tiles: records, fp16 rows of the cache, the chunk as far as the tile's last row sees it ----
   const int tile_rec = a.tile_rec;
@@ -338,97 +431,128 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
   // ---- records ----
   const int r_end = t_end < nt_rec ? t_end : nt_rec;
   if (t_first < r_end) {
-    const int pieces = a.rec_bytes >> 4;      // 16-byte pieces of a record
-    int pr[3], po[3], kind[3];                  // this thread's pieces of a tile: record, byte in it, plane
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const int i = tid + kChunkThreads * k;
-      pr[k] = i / pieces;
-      po[k] = (i - pr[k] * pieces) * 16;
-      const int es = po[k] - a.off_v_s, ez = po[k] - a.off_v_z, plane = a.R * a.NVG * 2;
-      kind[k] = es >= 0 && es < plane ? 1 : ez >= 0 && ez < plane ? 2 : 0;
-    }
-    const int32_t* table = a.table ? a.table + (size_t)b * a.NB : nullptr;
-    const int nvg_bits = 31 - __builtin_clz(a.NVG);
+    typedef __attribute__((address_space(4))) const int32_t* scalar_ptr;      // (through the scalar cache: see chunk_few.h)
     auto tile_count = [&](int t) { const int left = n_rec - t * tile_rec; return left < tile_rec ? left : tile_rec; };
-    auto record = [&](int blk) {
-      return a.blocks + (table ? (size_t)table[blk] * Hkv + j : (size_t)p * a.NB + blk) * a.rec_bytes;
+    auto record = [&](int blk) __attribute__((always_inline)) {
+      ArgsIn& a = args_here();
+      const scalar_ptr table = (scalar_ptr)(uintptr_t)(a.table + (size_t)b * a.NB);
+      return (const unsigned char*)a.blocks + (a.table ? (size_t)table[blk] * Hkv + j : (size_t)p * a.NB + blk) * a.rec_bytes;
     };
-    uint4 raw[3];
-    auto fetch = [&](int t) {
-      const int cnt = tile_count(t);
+    uint4 raw[3];      // this thread's 16-byte pieces of a tile on their way: pieces tid, tid + 512 and tid + 1024 of its records
+    static_assert(kMaxRec <= 3 * 16 * kChunkThreads && kChunkRecords == 4, "three pieces to a thread; record_of");
+    int listed[2];     // wavefront w: entries of record w's list
+    auto record_of = [](int i, int pieces) { return (i >= pieces) + (i >= 2 * pieces) + (i >= 3 * pieces); };
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+      ArgsIn& a = args_here();
+      const int cnt = tile_count(t), pieces = a.rec_bytes >> 4, tid = tid_here();
+      const unsigned char* mine = record(t * tile_rec + (wave < cnt ? wave : 0));      // wavefront w: record w
+      if (tile_rec == 1) {
+        const uint4* at = reinterpret_cast<const uint4*>(mine);
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (pr[k] < cnt) raw[k] = *reinterpret_cast<const uint4*>(record(t * tile_rec + pr[k]) + po[k]);
+        for (int k = 0; k < 3; ++k) raw[k] = at[tid + kChunkThreads * k < pieces ? tid + kChunkThreads * k : 0];
+      } else {
+        const unsigned char* from[kChunkRecords];
+#pragma unroll
+        for (int r = 0; r < kChunkRecords; ++r) from[r] = record(t * tile_rec + (r < cnt ? r : 0)) - r * a.rec_bytes;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {      // (pieces that the tile does not have: its first one once more)
+          const int i = tid + kChunkThreads * k < cnt * pieces ? tid + kChunkThreads * k : 0;
+          const unsigned char* at = i < pieces ? from[0] : i < 2 * pieces ? from[1] : i < 3 * pieces ? from[2] : from[3];
+          raw[k] = *reinterpret_cast<const uint4*>(at + i * 16);
+        }
+      }
+      const int ks = a.k4 + a.k16, lane = tid & 63;
+      listed[0] = mine[a.off_idx + (lane < ks ? lane : 0)];
+      listed[1] = mine[a.off_idx + (lane + 64 < ks ? lane + 64 : 0)];
     };
-    auto stage = [&](int t) {
-      const int cnt = tile_count(t);
+    // The planes of the keys, or of the values.
+    auto stage = [&](int t, bool values) __attribute__((always_inline)) {
+      ArgsIn& a = args_here();
+      const int cnt = tile_count(t), nvg_bits = a.nvg_bits, pieces = a.rec_bytes >> 4, plane = a.R * 2 << nvg_bits, tid = tid_here();
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        if (pr[k] >= cnt) continue;
-        if (kind[k] == 0) {
-          *reinterpret_cast<uint4*>(lds + kOffRaw + pr[k] * a.rec_bytes + po[k]) = raw[k];
+        const int i = tid + kChunkThreads * k, rec = record_of(i, pieces), po = (i - rec * pieces) << 4;
+        if (i >= cnt * pieces || (po >= a.off_v) != values) continue;
+        const int es = po - a.off_v_s, ez = po - a.off_v_z;
+        const bool scale = es >= 0 && es < plane, zero = ez >= 0 && ez < plane;
+        if (!scale && !zero) {
+          *reinterpret_cast<uint4*>(lds + kOffRaw + rec * a.rec_bytes + po) = raw[k];
         } else {      // value scales (zero-points): [token][group] there, [group][token] here
-          const int li = (po[k] - (kind[k] == 1 ? a.off_v_s : a.off_v_z)) >> 1;
-          unsigned short* to = reinterpret_cast<unsigned short*>(lds + kOffScale) + (kind[k] == 1 ? 0 : 8 * kScaleRow) + pr[k] * a.R;
+          const int li = (scale ? es : ez) >> 1;
+          if (nvg_bits == 0) {
+            *reinterpret_cast<uint4*>(lds + kOffScale + ((scale ? 0 : 8 * kScaleRow) + rec * a.R + li) * 2) = raw[k];
+            continue;
+          }
+          unsigned short* to = reinterpret_cast<unsigned short*>(lds + kOffScale) + (scale ? 0 : 8 * kScaleRow) + rec * a.R;
           const unsigned v[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int tok = (li + e) >> nvg_bits, vg = (li + e) & (a.NVG - 1);
+            const int tok = (li + e) >> nvg_bits, vg = (li + e) & ((1 << nvg_bits) - 1);
             if (tok < a.R) to[vg * kScaleRow + tok] = (unsigned short)(v[e >> 1] >> (16 * (e & 1)));
           }
         }
       }
     };
     // Wavefront w lists record w's 2-bit channels: place -> row of the key tile (twisted), 128 for places without a channel.
-    const int ks = a.k4 + a.k16;
     auto map_of = [&](int t) { return reinterpret_cast<unsigned short*>(lds + kOffMap) + (t & 1) * kChunkRecords * kD; };
-    auto list_channels = [&](int t) {
+    auto list_channels = [&](int t) __attribute__((always_inline)) {
       if (wave >= tile_count(t)) return;
-      const uint8_t* idx = record(t * tile_rec + wave) + a.off_idx;
-      unsigned long long low = ~0ull, high = ~0ull;      // channels 0 .. 63 and 64 .. 127 that are in no list
-      const int e0 = lane < ks ? idx[lane] : 255, e1 = lane + 64 < ks ? idx[lane + 64] : 255;
-      for (int e = 0; e < ks; ++e) {
-        const int ch = e < 64 ? __builtin_amdgcn_readlane(e0, e) : __builtin_amdgcn_readlane(e1, e - 64);
-        if (ch < 64) low &= ~(1ull << ch);
-        else if (ch < 128) high &= ~(1ull << (ch - 64));
-      }
-      unsigned short* to = map_of(t) + wave * kD;
+      ArgsIn& a = args_here();
+      const int ks = a.k4 + a.k16, lane = tid_here() & 63;
+      volatile unsigned short* to = map_of(t) + wave * kD;      // (one wavefront's reads and writes of the LDS keep their order)
+      to[lane] = 1;
+      to[lane + 64] = 1;
+      if (lane < ks && listed[0] < kD) to[listed[0]] = 0;
+      if (lane + 64 < ks && listed[1] < kD) to[listed[1]] = 0;
+      const unsigned long long low = __ballot(to[lane] != 0), high = __ballot(to[lane + 64] != 0), before = (1ull << lane) - 1;
       const int n_low = __popcll(low), n = n_low + __popcll(high);
-      const unsigned long long before = (1ull << lane) - 1;
       if (low >> lane & 1) to[__popcll(low & before)] = (unsigned short)(lane << 8 | twist(lane) << 4);
       if (high >> lane & 1) to[n_low + __popcll(high & before)] = (unsigned short)((lane + 64) << 8 | twist(lane + 64) << 4);
       for (int i = n + lane; i < kD; i += 64) to[i] = (unsigned short)(kD << 8);
     };
 
+    auto tokens_of = [&](int t) { return tile_count(t) * a.R; };
     fetch(t_first);
     list_channels(t_first);
-    stage(t_first);
+    stage(t_first, false);
+    stage(t_first, true);
     if (t_first + 1 < r_end) fetch(t_first + 1);
     __syncthreads();
-    if (wave < 4) unpack_keys(lds, a, 0, map_of(t_first), tile_count(t_first) * a.R);
-    else unpack_values(lds, a, kKeyBytes, tile_count(t_first) * a.R);
-    if (t_first + 1 < r_end) list_channels(t_first + 1);
+    if (wave < 4) unpack_keys(lds, 0, map_of(t_first), tokens_of(t_first));
+    else unpack_values(lds, kKeyBytes, tokens_of(t_first));
     __syncthreads();
-    for (int t = t_first; t < r_end; ++t) {
-      const bool next = t + 1 < r_end;
-      const int here = (t - t_first & 1) * kTileBytes, there = kTileBytes - here;
-      if (next) stage(t + 1);
-      __syncthreads();
-      if (t + 2 < r_end) fetch(t + 2);
-      // The wavefronts of a SIMD (w and w + 4) unpack the next tile at different times: one's vector instructions run beside
-      // the other's matrix instructions.
-      if (next && wave < 4) unpack_keys(lds, a, there, map_of(t + 1), tile_count(t + 1) * a.R);
-      if (active) {
-        const int n_tok = tile_count(t) * a.R;
-#pragma unroll 1
-        for (int s = share * kSlices; s < (share + 1) * kSlices && s * 32 < n_tok; s += kStep)
-          attend<kStep, true, true>(lds, here, here + kKeyBytes, s, st, c, (s + kStep) * 32 > n_tok, n_tok);
-      }
-      if (next && wave >= 4) unpack_values(lds, a, there + kKeyBytes, tile_count(t + 1) * a.R);
-      if (t + 2 < r_end) list_channels(t + 2);
-      __syncthreads();
+    if (t_first + 1 < r_end) {
+      stage(t_first + 1, false);
+      list_channels(t_first + 1);
     }
+    Pipe<true> in;
+    if (active) begin<true>(lds, in, tokens_of(t_first), tokens_of(t_first), c, sc[0], pw[1], st);
+    for (int t = t_first; t < r_end; ++t) {
+      const bool next = t + 1 < r_end, next2 = t + 2 < r_end;
+      const int here = (t - t_first & 1) * kTileBytes, there = kTileBytes - here, n_tok = tokens_of(t), n_next = next ? tokens_of(t + 1) : 0;
+      __syncthreads();      // this tile's values are there, and the next one's keys are staged
+      if (next) stage(t + 1, true);
+      if (next2) fetch(t + 2);
+      // The wavefronts of a SIMD (w and w + 4) unpack at different times: one's vector instructions run beside the other's matrix
+      // instructions.
+      if (next && wave < 4) unpack_keys(lds, there, map_of(t + 1), tokens_of(t + 1));
+      if (active) {
+        step<0>(lds, in, t == t_first ? 0 : here - there, sc[0], sc[1], pw[1], pw[0], 2 * 32 > n_tok, n_tok, c, st);
+        step<1>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 3 * 32 > n_tok, n_tok, c, st);
+      }
+      __syncthreads();      // the next tile's keys are there, and its values are staged
+      if (next2) {
+        stage(t + 2, false);
+        list_channels(t + 2);
+      }
+      if (next && wave >= 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1));
+      if (active) {         // (behind the last tile: scores of what the other tile's place holds, all of them hidden)
+        step<2>(lds, in, there - here, sc[0], sc[1], pw[1], pw[0], 4 * 32 > n_tok, n_tok, c, st);
+        step<3>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 32 > n_next, n_next, c, st);
+      }
+    }
+    if (active) finish(lds, in, pw[1], st);
+    __syncthreads();
   }
 
   // ---- fp16 rows: the cache's (all of them are seen), then the chunk's (causal) ----
@@ -436,52 +560,67 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
   if (f_first < t_end) {
     const int prow = tid >> 4, piece = tid & 15;
     const int place = prow * kRowBytes + ((piece ^ twist(prow)) << 4);      // of this thread's first piece; the others 32 rows on
-    uint4 fk[4], fv[4];
-    auto fetch = [&](int t) {
+    uint4 held[4];                            // half of the next tile on its way: its keys, then its values
+    auto fetch = [&](int t, bool keys) {
       const bool win = t < nt_rec + nt_win;
       const int first = (t - nt_rec - (win ? 0 : nt_win)) * kChunkTile, n = win ? n_fp16 : seen;
-      const __half* k = win ? a.res_k + (size_t)p * a.RW * kD : a.k + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
-      const __half* v = win ? a.res_v + (size_t)p * a.RW * kD : a.v + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
-      const int64_t step = win ? kD : a.kvs.t;
+      const __half* from = win ? (keys ? a.res_k : a.res_v) + (size_t)p * a.RW * kD : (keys ? a.k : a.v) + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
+      const int step = win ? kD : (int)a.kvs.t;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         int r = first + prow + 32 * i;
         r = r < n ? r : n - 1;      // places behind the last row hold that row once more: finite, and masked
-        fk[i] = *reinterpret_cast<const uint4*>(k + r * step + piece * 8);
-        fv[i] = *reinterpret_cast<const uint4*>(v + r * step + piece * 8);
+        held[i] = *reinterpret_cast<const uint4*>(from + (int64_t)r * step + piece * 8);
       }
     };
-    auto stage = [&](int t, int at) {
-      const bool convert = bf16 && t >= nt_rec + nt_win;
+    auto store = [&](int t, int at) {
+      if (bf16 && t >= nt_rec + nt_win) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        *reinterpret_cast<uint4*>(lds + at + place + i * 32 * kRowBytes) = as_f16x8(fk[i], convert);
-        *reinterpret_cast<uint4*>(lds + at + kKeyBytes + place + i * 32 * kRowBytes) = as_f16x8(fv[i], convert);
+        for (int i = 0; i < 4; ++i) held[i] = as_f16x8(held[i], true);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(lds + at + place + i * 32 * kRowBytes) = held[i];
     };
-    fetch(f_first);
-    stage(f_first, 0);
+    fetch(f_first, true);
+    store(f_first, 0);
+    fetch(f_first, false);
+    store(f_first, kKeyBytes);
     __syncthreads();
+    Pipe<false> in;
+    auto first_of = [&](int t) { return (t - nt_rec - (t < nt_rec + nt_win ? 0 : nt_win)) * kChunkTile; };
+    // Tokens of the tile that a row sees, and those that all rows of the wavefront see.
+    auto limit_of = [&](int t) { return (t < nt_rec + nt_win ? n_fp16 : token + 1) - first_of(t); };
+    auto all_of = [&](int t) { return (t < nt_rec + nt_win ? n_fp16 : see_min) - first_of(t); };
+    if (active) begin<false>(lds, in, all_of(f_first), limit_of(f_first), c, sc[0], pw[1], st);
     for (int t = f_first; t < t_end; ++t) {
+      const bool next = t + 1 < t_end;
       const int here = (t - f_first & 1) * kTileBytes, there = kTileBytes - here;
-      if (t + 1 < t_end) fetch(t + 1);
+      const int all = all_of(t), limit = limit_of(t);
+      __syncthreads();      // this tile's values are there
+      if (next) fetch(t + 1, true);
       if (active) {
-        const bool win = t < nt_rec + nt_win;
-        const int first = (t - nt_rec - (win ? 0 : nt_win)) * kChunkTile;
-        const int lim_min = (win ? n_fp16 : see_min) - first, lim_max = (win ? n_fp16 : see_max) - first;
-        const int limit = (win ? n_fp16 : token + 1) - first;
-#pragma unroll 1
-        for (int s = share * kSlices; s < (share + 1) * kSlices && s * 32 < lim_max; s += kStep)
-          attend<kStep, false, false>(lds, here, here + kKeyBytes, s, st, c, (s + kStep) * 32 > lim_min, limit);
+        step<0>(lds, in, t == f_first ? 0 : here - there, sc[0], sc[1], pw[1], pw[0], 2 * 32 > all, limit, c, st);
+        step<1>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 3 * 32 > all, limit, c, st);
       }
-      if (t + 1 < t_end) stage(t + 1, there);
-      __syncthreads();
+      if (next) {
+        store(t + 1, there);
+        fetch(t + 1, false);
+      }
+      __syncthreads();      // the next tile's keys are there
+      if (active) {
+        const int all_next = next ? all_of(t + 1) : 0, limit_next = next ? limit_of(t + 1) : 0;
+        step<2>(lds, in, there - here, sc[0], sc[1], pw[1], pw[0], 4 * 32 > all, limit, c, st);
+        step<3>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 32 > all_next, limit_next, c, st);
+      }
+      if (next) store(t + 1, there + kKeyBytes);
     }
+    if (active) finish(lds, in, pw[1], st);
+    __syncthreads();
   }
 
-  // ---- the shares of a row meet in LDS; results leave in whole rows ----
-  float* const meet = reinterpret_cast<float*>(lds);                       // [wavefront][32][kOutRow]
-  float2* const ml = reinterpret_cast<float2*>(lds + 8 * 32 * kOutRow * 4);   // [wavefront][32]
+  // ---- results leave in whole rows, by way of LDS ----
+  float* const meet = reinterpret_cast<float*>(lds);                       // [kRows][kOutRow]
+  float2* const ml = reinterpret_cast<float2*>(lds + kRows * kOutRow * 4);    // [kRows]
   {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
     st.l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
@@ -499,20 +638,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
   for (int r = tid >> 4; r < kRows; r += kChunkThreads / 16) {      // 16 threads to a row
     const int rr = rt * kRows + r;
     if (rr >= n_rows) break;
-    const int w0 = r >> 5, in_group = r & 31;
-    float m = -INFINITY;
-#pragma unroll
-    for (int s = 0; s < kShares; ++s) m = fmaxf(m, ml[(s * ROW_GROUPS + w0) * 32 + in_group].x);
-    float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < kShares; ++s) {
-      const int at = (s * ROW_GROUPS + w0) * 32 + in_group;
-      const float2 x = ml[at];
-      const float f = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
-      sum += f * x.y;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += f * meet[at * kOutRow + chan + e];
-    }
+    const float m = ml[r].x, sum = ml[r].y, *o = meet + r * kOutRow + chan;
     if (a.split) {
       const size_t slot = ((size_t)blockIdx.x * gridDim.y + rt) * kRows + r;
       float* to = a.part + slot * kD + chan;
@@ -547,14 +673,14 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, Counts co
   if (rr >= n_rows || at.b != a.b0 + i) return;      // (a sequence without new tokens has no unit)
   const size_t first = ((size_t)at.first_block * a.row_tiles + rr / rows) * rows + rr % rows, step = (size_t)a.Hkv * a.row_tiles * rows;
   const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)blocks * rows * kD);
-  float m = -INFINITY, sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  float m = kNoToken, sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int s = 0; s < at.n_splits; ++s) m = fmaxf(m, ml[first + s * step].x);
 #pragma unroll 4
   for (int s = 0; s < at.n_splits; ++s) {
     const size_t slot = first + s * step;
     const float2 x = ml[slot];
-    const float f = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - m);
+    const float f = __builtin_amdgcn_exp2f(x.x - m);
     const f4 u = *reinterpret_cast<const f4*>(a.part + slot * kD + chan), v = *reinterpret_cast<const f4*>(a.part + slot * kD + chan + 4);
     sum += f * x.y;
 #pragma unroll
@@ -609,18 +735,16 @@ hipError_t start_chunk_few_1(const ChunkArgs& a, const ChunkCounts* c, int units
 hipError_t start_chunk_few_2(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
 hipError_t start_chunk_few_3(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
 
-template <int ROW_GROUPS>
 static hipError_t start_tiles(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s) {
   const dim3 grid(units * a.Hkv, a.row_tiles);
-  if (c) chunk_attention_kernel<ROW_GROUPS, ChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, *c);
-  else chunk_attention_kernel<ROW_GROUPS, NoChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, NoChunkCounts{});
+  if (c) chunk_attention_kernel<ChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, *c);
+  else chunk_attention_kernel<NoChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, NoChunkCounts{});
   return hipGetLastError();
 }
 
 hipError_t launch_chunk(const ChunkArgs& a, const ChunkCounts* c, int units, int n_seq, bool few, int rows, hipStream_t s) {
-  hipError_t e;
-  if (few) e = rows == 16 ? start_chunk_few_1(a, c, units, s) : rows == 32 ? start_chunk_few_2(a, c, units, s) : start_chunk_few_3(a, c, units, s);
-  else e = rows == 64 ? start_tiles<2>(a, c, units, s) : rows == 128 ? start_tiles<4>(a, c, units, s) : start_tiles<8>(a, c, units, s);
+  const hipError_t e = !few ? start_tiles(a, c, units, s) : rows == 16 ? start_chunk_few_1(a, c, units, s) : rows == 32 ? start_chunk_few_2(a, c, units, s)
+                                                                                                           : start_chunk_few_3(a, c, units, s);
   if (e != hipSuccess || !a.split) return e;
   const int per_pair = (a.row_tiles * rows + 15) / 16, blocks = units * a.Hkv * a.row_tiles;
   if (c) chunk_merge_kernel<<<per_pair * n_seq * a.Hkv, 256, 0, s>>>(a, *c, rows, blocks, per_pair);
