@@ -9,7 +9,7 @@ namespace mixkvq {
 
 constexpr int kChunkUnitsAtOnce = 256;      // one workgroup to a compute unit (its tiles fill the LDS)
 constexpr int kChunkMaxNew = 1 << 20;
-constexpr int kFewRows = 96;                // query rows up to which the kernel for few rows is taken
+constexpr int kFewRows = 512;               // query rows up to which the kernel for few rows may be taken
 
 static int div_up(int a, int b) { return (a + b - 1) / b; }
 
@@ -32,52 +32,78 @@ static int splits_of(int steps, int chain) {
   return s > kChunkMaxSplits ? kChunkMaxSplits : s;
 }
 
-static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
+// The cut of a call for one kernel that takes the least time, and that time in microseconds.  A unit (one split of one tile of
+// rows) costs its steps and a constant part.  Workgroups of one length run in rounds; of several (later rows of a chunk see more
+// tokens, and the longest start first) they fill the compute units evenly until the shortest ones end.  Splits have to be merged,
+// which costs a launch and their rows' traffic.  The constants fit what was measured for cuts of 1 to 258 steps, e.g. few rows
+// (8 sequences of 32k): 17 steps a unit 69 us, 9 steps 88, 19 steps 73; tiles (1000 after 31000 tokens): 28 steps 653 us,
+// 14 steps 742, 126 steps 678; (8192 tokens, empty cache): unsplit 508 us, 32 steps 595.
+static double cut_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq, ChunkPlan* pl) {
+  static const int kTry[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64};
+  constexpr int kTries = sizeof kTry / sizeof kTry[0];
+  static_assert(kChunkMaxSplits == 64, "the last try");
   const mixkvq_config& cfg = c->v.cfg;
-  int most = 0;
-  for (int b = 0; b < cfg.B; ++b) most = n_new_of(n_seq, n_max, b) > most ? n_new_of(n_seq, n_max, b) : most;
-  ChunkPlan pl{};
-  const int rows = most * c->v.g;
-  pl.few = rows <= kFewRows && chunk_few_fits(c->v);
-  if (pl.few) pl.rows = rows <= 16 ? 16 : rows <= 32 || chunk_few_rows(c->v) == 32 ? 32 : 48;
-  else pl.rows = 256;
-  // The splits' length that takes the least time, counted in steps.  A unit costs its steps and a constant part.  Workgroups
-  // of one length run in rounds; of several (later rows of a chunk see more tokens, and the longest start first) they fill the
-  // compute units evenly until the shortest ones end.  Splits have to be merged, which costs a launch and their rows' traffic.
-  const int fixed = pl.few ? 3 : 2;
-  int longest = 1, shortest = 1 << 30;
+  const int fixed = pl->few ? 6 : 2;
+  const double step_us = pl->few ? 2.5 : 4.8;
+  int longest = 1, shortest = 1 << 30, chain[kTries];
   bool equal = true;      // (the longest start first only among a sequence's own row tiles)
-  for (int b = 0; b < cfg.B; ++b) {
-    const int n = n_new_of(n_seq, n_max, b);
-    if (!n) continue;
-    const int t = chunk_steps(c, pl.few, b, n), t0 = chunk_steps(c, pl.few, b, 1);
-    equal = equal && (longest == 1 || t == longest);
-    longest = t > longest ? t : longest;
-    shortest = t0 < shortest ? t0 : shortest;
+  int64_t units[kTries] = {};
+  double steps = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int b = 0; b < cfg.B;) {
+      const int n = n_new_of(n_seq, n_max, b);
+      int same = 1;      // sequences with the same counts from here on
+      while (b + same < cfg.B && n_new_of(n_seq, n_max, b + same) == n && c->seq[b + same] == c->seq[b]) ++same;
+      if (n) {
+        const int t = chunk_steps(c, pl->few, b, n);
+        if (pass == 0) {
+          const int t0 = chunk_steps(c, pl->few, b, 1);
+          equal = equal && (longest == 1 || t == longest);
+          longest = t > longest ? t : longest;
+          shortest = t0 < shortest ? t0 : shortest;
+        } else {
+          const int64_t tiles = (int64_t)same * cfg.Hkv * div_up(n * c->v.g, pl->rows);
+          const int first = pl->rows / c->v.g + 1;
+          for (int i = 0; i < kTries; ++i) units[i] += tiles * splits_of(t, chain[i]);
+          steps += (double)tiles * (t + (n > first ? chunk_steps(c, pl->few, b, first) : t)) / 2;
+        }
+      }
+      b += same;
+    }
+    if (pass == 0)
+      for (int i = 0; i < kTries; ++i) chain[i] = div_up(longest, kTry[i]);
   }
   double best = 0;
-  pl.chain = longest;
-  for (int s = 1; s <= kChunkMaxSplits && s <= longest; ++s) {
-    const int chain = div_up(longest, s);
-    if (s > 1 && chain == div_up(longest, s - 1)) continue;
-    int64_t units = 0;
-    double steps = 0;
-    for (int b = 0; b < cfg.B; ++b) {
-      const int n = n_new_of(n_seq, n_max, b);
-      if (!n) continue;
-      const int64_t tiles = (int64_t)cfg.Hkv * div_up(n * c->v.g, pl.rows);
-      units += tiles * splits_of(chunk_steps(c, pl.few, b, n), chain);
-      steps += (double)tiles * (chunk_steps(c, pl.few, b, n) + chunk_steps(c, pl.few, b, n < pl.rows / c->v.g ? n : pl.rows / c->v.g + 1)) / 2;
-    }
-    const double rounds = (double)((units + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain + fixed);
-    const double even = (steps + (double)fixed * units) / kChunkUnitsAtOnce + (equal && shortest < chain ? shortest : chain) + fixed;
-    const double t = (rounds < even ? rounds : even) + (s > 1 ? fixed + units * pl.rows / 32768.0 : 0);
-    if (s == 1 || t < best) {
+  for (int i = 0; i < kTries && kTry[i] <= longest; ++i) {
+    const double rounds = (double)((units[i] + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain[i] + fixed);
+    const double even = (steps + (double)fixed * units[i]) / kChunkUnitsAtOnce + (equal && shortest < chain[i] ? shortest : chain[i]) + fixed;
+    // (rounds are exact if there is one; of units of one length they are a bound from above, else hopeful)
+    const bool less = units[i] <= kChunkUnitsAtOnce || (equal ? rounds < even : rounds > even);
+    const double t = ((less ? rounds : even) + (i ? 2 + units[i] * pl->rows / 32768.0 : 0)) * step_us;
+    if (i == 0 || t < best) {
       best = t;
-      pl.chain = chain;
+      pl->chain = chain[i];
     }
   }
-  return pl;
+  return best;
+}
+
+// The kernel for few rows reads every record anew for each 16, 32 or 48 of them, the one with tiles of 256 rows dequantizes it once in
+// LDS.  Where the second starts to win depends on the compute units that each leaves idle: 24 sequences of 8k tokens, 161
+// rows, 297 and 195 us; 8 of 16k, 161 rows, 106 and 118 us, 196 rows, 148 and 121 us; one of 32k, 259 rows, 58 and 78 us.
+static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
+  int most = 0;
+  for (int b = 0; b < c->v.cfg.B; ++b) most = n_new_of(n_seq, n_max, b) > most ? n_new_of(n_seq, n_max, b) : most;
+  const int rows = most * c->v.g;
+  ChunkPlan tiles{false, 256, 1}, few{true, rows <= 16 ? 16 : rows <= 32 || chunk_few_rows(c->v) == 32 ? 32 : 48, 1};
+  const bool fits = chunk_few_fits(c->v);
+  if (!fits || rows > kFewRows) {
+    cut_chunk(c, n_max, n_seq, &tiles);
+    return tiles;
+  }
+  const double few_us = cut_chunk(c, n_max, n_seq, &few);
+  if (rows <= 48) return few;
+  return few_us <= cut_chunk(c, n_max, n_seq, &tiles) ? few : tiles;
 }
 
 // Sequences [b0, b0 + n) of the call as one launch (counts that differ in *c).  How many sequences a launch takes is up to the
