@@ -357,6 +357,8 @@ class Cache:
         assert (B, Hq, D) == (cfg.B, cfg.Hq, cfg.D) and k_new.shape == (B, cfg.Hkv, n, D) == v_new.shape
         dt = torch.bfloat16 if cfg.in_dtype else torch.float16
         assert k_new.stride() == v_new.stride() and q.dtype == k_new.dtype == v_new.dtype == dt
+        at = self.device.index or 0
+        assert q.get_device() == k_new.get_device() == v_new.get_device() == at
         counts = None
         if n_seq is not None:
             assert len(n_seq) == B
@@ -366,12 +368,13 @@ class Cache:
                 out = torch.empty_like(q)
             if lse is None:
                 lse = torch.empty((B, Hq, n), dtype=torch.float32, device=self.device)
-            assert out.shape == q.shape and out.dtype == dt
-            assert lse.shape == (B, Hq, n) and lse.dtype == torch.float32 and lse.is_contiguous()
+            assert out.shape == q.shape and out.dtype == dt and out.get_device() == at
+            assert lse.shape == (B, Hq, n) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == at
             need = self.lib.mixkvq_chunk_workspace(self.handle, n, counts)
             _check(min(need, 0))
             if workspace is None and need:
                 workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            assert workspace is None or (workspace.get_device() == at and workspace.is_contiguous())
             wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
             _check(self.lib.mixkvq_chunk_attention(self.handle, q.data_ptr(), _strides3(q), k_new.data_ptr(), v_new.data_ptr(),
                                                    _strides3(k_new), n, counts, out.data_ptr(), _strides3(out), lse.data_ptr(),
@@ -430,8 +433,10 @@ def verify_draft(p_target, draft, u_accept, u_next, p_draft=None, n_seq=None, n_
     if p_draft is not None:
         assert p_draft.shape == (B, n, V) and p_draft.dtype == torch.float32 and (p_draft.numel() == 0 or p_draft.stride(2) == 1)
     if n_seq is not None:
-        assert n_seq.shape == (B,) and n_seq.dtype == torch.int32 and n_seq.is_contiguous() and n_seq.is_cuda
-    device = p_target.device
+        assert n_seq.shape == (B,) and n_seq.dtype == torch.int32 and n_seq.is_contiguous()
+    device, at = p_target.device, p_target.get_device()
+    assert at == draft.get_device() == u_accept.get_device() == u_next.get_device()
+    assert all(t is None or t.get_device() == at for t in (p_draft, n_seq, n_accepted, tokens, workspace))
     with _on(device, stream):
         if n_accepted is None:
             n_accepted = torch.empty(B, dtype=torch.int32, device=device)
@@ -443,6 +448,7 @@ def verify_draft(p_target, draft, u_accept, u_next, p_draft=None, n_seq=None, n_
         _check(min(need, 0))
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        assert workspace.is_contiguous()
         _check(lib.mixkvq_verify_draft(B, n, V, p_target.data_ptr(), _I64x2(p_target.stride(0), p_target.stride(1)),
                                        None if p_draft is None else p_draft.data_ptr(),
                                        None if p_draft is None else _I64x2(p_draft.stride(0), p_draft.stride(1)),

@@ -168,20 +168,21 @@ __device__ __forceinline__ float largest(const f16v& s) {
 }
 
 // Brings the sums and the weights that are still to be used to a new reference if a score (mx: this lane's largest) has run too far
-// ahead; only then do the two lanes of a row agree on it.  References are whole numbers: the weights' factor is a power of two.
+// ahead; only then do the two lanes of a row agree on it.  References are whole numbers: the weights' factor is a power of two, taken
+// in two parts because a weight of up to 2^13 may still count when the whole factor is below binary16.
 __device__ __forceinline__ void follow(float mx, Rows& st, h8 (&p)[2]) {
   if (__any(mx > st.m + kHeadroom)) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    const float m = ceilf(fmaxf(st.m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])))), f = __builtin_amdgcn_exp2f(st.m - m);
+    const float m = ceilf(fmaxf(st.m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])))), back = st.m - m, f = __builtin_amdgcn_exp2f(back);
     st.m = m;
     st.l *= f;
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[b][r] *= f;
-    const _Float16 f16 = (_Float16)f;
+    const _Float16 f0 = (_Float16)__builtin_amdgcn_exp2f(fmaxf(back, -14.f)), f1 = (_Float16)__builtin_amdgcn_exp2f(fminf(back + 14.f, 0.f));
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p[i] *= h8{f16, f16, f16, f16, f16, f16, f16, f16};
+    for (int i = 0; i < 2; ++i) p[i] = p[i] * h8{f0, f0, f0, f0, f0, f0, f0, f0} * h8{f1, f1, f1, f1, f1, f1, f1, f1};
   }
 }
 
