@@ -29,7 +29,10 @@ constexpr int kScaleRow = kChunkTile + 8;                        // halves per v
 constexpr int kOffRaw = 2 * kTileBytes;
 constexpr int kOffScale = kOffRaw + kMaxRec;                     // [8][kScaleRow] scales, then zero-points
 constexpr int kOffMap = kOffScale + 2 * 8 * kScaleRow * 2;       // [2][kChunkRecords][128] rows of the tile by channel place
-constexpr int kLdsBytes = kOffMap + 2 * kChunkRecords * kD * 2;
+constexpr int kOffPick = kOffMap + 2 * kChunkRecords * kD * 2;    // [9] halves: 1 in place 0 .. 7, and nowhere
+constexpr int kLdsBytes = kOffPick + 9 * 16;
+// What binary16 drops of the 4-bit tier's keys: a row per list entry, twice (two tiles), where records leave room for it.
+constexpr int kRestRows = 16, kRestBytes = kRestRows * kRowBytes, kOffRest = kOffScale - 2 * kRestBytes;
 static_assert(kLdsBytes <= 160 * 1024, "LDS of a compute unit");
 constexpr int kOutRow = kD + 4;                                  // floats of a row where the wavefronts' results meet
 constexpr int kRows = 256;                                        // query rows of a workgroup: 32 to a wavefront
@@ -65,6 +68,14 @@ __device__ __forceinline__ unsigned dequant(unsigned w, const unsigned (&mask)[5
   const unsigned x = C::kShift == C::kUp ? w : w >> (C::kShift - C::kUp);
   const _Float16 off = (_Float16)(float)(1 << (10 - C::kUp));
   return as_u((as_h2((x & mask[C::kUp / BITS]) | C::kMagic) - h2{off, off}) * s + z);
+}
+// What `k` drops of two 4-bit codes times s plus z: exact products and sums of binary32 (15 bits, and 11 at not too far an exponent).
+template <int I>
+__device__ __forceinline__ unsigned dropped(unsigned w, unsigned k, h2 s, h2 z) {
+  const h2 h = as_h2(k), sz = s, zz = z;
+  const float c0 = (float)((w >> (4 * I)) & 15u), c1 = (float)((w >> (16 + 4 * I)) & 15u);
+  const float r0 = __builtin_fmaf(c0, (float)sz[0], (float)zz[0]) - (float)h[0], r1 = __builtin_fmaf(c1, (float)sz[1], (float)zz[1]) - (float)h[1];
+  return as_u(__builtin_convertvector(f2{r0, r1}, h2));
 }
 __device__ __forceinline__ unsigned in_vgpr(unsigned x) {
   asm("" : "+v"(x));
@@ -191,17 +202,67 @@ template <bool BY_CHANNEL>
 struct Pipe {
   Operands<BY_CHANNEL> at;
   h8 k[4], v[4];      // the next operands of the two products: a ring, each refilled four matrix instructions ahead
+  h8 q;               // queries at the channels of the 4-bit list, entries 8 half ..
+  int entry;          // this lane's entry of that list
 };
+
+// The queries at a list's channels, as the ninth operand of a slice's scores: a product with ones at (entry, channel), which is
+// exact.  entry: the channel of entry 8 (m / 4 % 2) + 4 (m / 8) + m % 4 in lane m < 16 (and m + 32), no channel elsewhere.
+__device__ __forceinline__ h8 pick_queries(unsigned char* lds, int entry, const Rows& st) {
+  f16v d;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) d[r] = 0.f;
+  const unsigned from = entry - 8 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const unsigned at = from - 16 * i;
+    d = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_h8(lds, kOffPick + (at < 8 ? at : 8) * 16), st.q[i], d, 0, 0, 0);
+  }
+  h8 q;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) q[r] = (_Float16)d[r];
+  return q;
+}
+
+// Entries of a staged tile's 4-bit lists for pick_queries, a byte for each slice (255: none).
+__device__ __forceinline__ unsigned list_entries(const unsigned char* lds, int n_rec) {
+  ArgsIn& a = args_here();
+  const int m = tid_here() & 31, e = 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3);
+  unsigned all = 0;
+#pragma unroll
+  for (int slice = 0; slice < 4; ++slice) {
+    const int rec = 32 * slice * a.inv_r >> 16;
+    const bool there = rec < n_rec && m < 16 && e < a.k4;
+    const unsigned c = lds[kOffRaw + (there ? rec * a.rec_bytes + a.off_idx + a.k16 + e : 0)];
+    all |= (there ? c : 255u) << (8 * slice);
+  }
+  return all;
+}
+
+__device__ __forceinline__ void take_list(unsigned char* lds, Pipe<true>& in, unsigned entries, int slice, const Rows& st) {
+  const int entry = entries >> (8 * slice) & 255;
+  if (__any(entry != in.entry)) {      // (lists change slowly)
+    in.entry = entry;
+    in.q = pick_queries(lds, entry, st);
+  }
+}
 
 // One step of a wavefront, on three slices at once: the scores of slice SLICE + 1 are formed (`next`), those of slice SLICE (`cur`, hidden
 // and followed) become weights (`p`), and the values of the slice before are added with its weights (`before`).  Nothing of
 // this depends on anything else of it, and the order is fixed piece by piece: every matrix instruction finds its operands in
 // registers and has a sixteenth of the vector instructions behind it, so that neither the LDS nor the exponentials are waited for.
-// Out: the next scores, hidden and followed.
-template <int SLICE, bool BY_CHANNEL>
-__device__ __forceinline__ void step(unsigned char* lds, Pipe<BY_CHANNEL>& in, int move, f16v& cur, f16v& next, const h8 (&before)[2], h8 (&p)[2],
+// Out: the next scores, hidden and followed.  REST: the scores have a ninth product, what binary16 drops of the 4-bit tier's keys (the rows
+// from rest on, less the keys' address) by the queries at its channels (entries).
+template <int SLICE, bool REST, bool BY_CHANNEL>
+__device__ __forceinline__ void step(unsigned char* lds, Pipe<BY_CHANNEL>& in, int move, int rest, unsigned entries, f16v& cur, f16v& next, const h8 (&before)[2], h8 (&p)[2],
                                      bool masked, int limit, float c, Rows& st) {
   float sum = 0.f, mx = 0.f;
+  h8 dropped;
+  if constexpr (REST) {
+    constexpr int kNext = (SLICE + 1) & 3;
+    take_list(lds, in, entries, kNext, st);
+    dropped = join(lds_column(lds, in.at.k[2 * kNext] + rest), lds_column(lds, in.at.k[2 * kNext + 1] + rest));
+  }
 #pragma unroll
   for (int r = 0; r < 16; ++r) next[r] = 0.f;
 #pragma unroll
@@ -226,6 +287,7 @@ __device__ __forceinline__ void step(unsigned char* lds, Pipe<BY_CHANNEL>& in, i
       p[e >> 2][2 * (e & 3) + 1] = w[1];
       ++e;
     }
+    if (REST && s == 10) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(dropped, in.q, next, 0, 0, 0);
     if (s == 14) mx = largest(next);
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -240,8 +302,8 @@ __device__ __forceinline__ void step(unsigned char* lds, Pipe<BY_CHANNEL>& in, i
 
 // What the first step takes: the first slice's scores, no weights, operands in the rings.  Rows see `limit` tokens of the tile, all of
 // them `all`.
-template <bool BY_CHANNEL>
-__device__ __forceinline__ void begin(unsigned char* lds, Pipe<BY_CHANNEL>& in, int all, int limit, float c, f16v& s, h8 (&p)[2], Rows& st) {
+template <bool REST, bool BY_CHANNEL>
+__device__ __forceinline__ void begin(unsigned char* lds, Pipe<BY_CHANNEL>& in, unsigned entries, int all, int limit, float c, f16v& s, h8 (&p)[2], Rows& st) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) in.k[i] = in.at.key(lds, 0, i);
 #pragma unroll
@@ -250,6 +312,11 @@ __device__ __forceinline__ void begin(unsigned char* lds, Pipe<BY_CHANNEL>& in, 
   for (int i = 0; i < 8; ++i) {
     s = __builtin_amdgcn_mfma_f32_32x32x16_f16(in.k[i & 3], st.q[i], s, 0, 0, 0);
     in.k[i & 3] = in.at.key(lds, i < 4 ? 0 : 1, (i + 4) & 7);
+  }
+  if constexpr (REST) {
+    in.entry = -1;
+    take_list(lds, in, entries, 0, st);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(join(lds_column(lds, in.at.k[0] + kOffRest), lds_column(lds, in.at.k[1] + kOffRest)), in.q, s, 0, 0, 0);
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) p[i] = h8{0, 0, 0, 0, 0, 0, 0, 0};
@@ -273,7 +340,9 @@ __device__ __forceinline__ void finish(unsigned char* lds, Pipe<BY_CHANNEL>& in,
 }
 
 // Dequantizes the staged tile's keys into `keys` (a row per channel).  Threads 0 .. 255; threads 256 .. 511 do the values.
-__device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, const unsigned short* map, int n_tok) {
+// REST: and what binary16 drops of the 4-bit tier into `rest` (a row per list entry).
+template <bool REST>
+__device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, int rest, const unsigned short* map, int n_tok) {
   ArgsIn& a = args_here();
   const int Rr = a.R, inv_r = a.inv_r, inv_gk = a.inv_gk, tid = tid_here();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -309,8 +378,8 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, const 
   }
   // Side tiers: their channels stand in the record's list, an unused entry (255) goes to the row that nobody reads.
   const int k4 = a.k4, k16 = a.k16;
-  for (int u = tid; u < a.W4 * 32; u += 256) {      // four bits: eight tokens of the four even or odd channels of a word
-    const int odd = u & 1, tg = (u >> 1) & 15, w = u >> 5, t = tg * 8;
+  for (int u = tid ^ 128; u < a.W4 * 64; u += 256) {      // four bits: eight tokens of two even or odd channels of a word
+    const int odd = u & 1, late = (u >> 1) & 1, tg = (u >> 2) & 15, w = u >> 6, t = tg * 8;
     if (t >= n_tok) continue;
     const int rec = t * inv_r >> 16, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
     const int words = raw + a.off_k4 + (tin * a.W4 + w) * 4;
@@ -319,19 +388,28 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, const 
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       x[i] = __builtin_amdgcn_perm(*reinterpret_cast<const unsigned*>(lds + words + (2 * i + 1) * a.W4 * 4),
-                                   *reinterpret_cast<const unsigned*>(lds + words + 2 * i * a.W4 * 4), pick);
-    const unsigned* s = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_s + ((tin * inv_gk >> 16) * k4 + 8 * w) * 2);
-    const unsigned* z = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_z + ((tin * inv_gk >> 16) * k4 + 8 * w) * 2);
-    const unsigned char* list = lds + raw + a.off_idx + k16 + 8 * w + odd;
+                                   *reinterpret_cast<const unsigned*>(lds + words + 2 * i * a.W4 * 4), pick) >> (8 * late);
+    const int first = 8 * w + 4 * late;      // list entries first + 2 I + odd
+    const unsigned* s = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_s + ((tin * inv_gk >> 16) * k4 + first) * 2);
+    const unsigned* z = reinterpret_cast<const unsigned*>(lds + raw + a.off_k4_z + ((tin * inv_gk >> 16) * k4 + first) * 2);
+    const unsigned char* list = lds + raw + a.off_idx + k16 + first + odd;
 #define MIXKVQ_CHANNEL(I)                                                                                                  \
   {                                                                                                                        \
     const h2 s2 = as_h2(__builtin_amdgcn_perm(s[I], s[I], twice)), z2 = as_h2(__builtin_amdgcn_perm(z[I], z[I], twice));   \
     const int ch = list[2 * I] < kD ? list[2 * I] : kD;                                                                    \
     const int to = keys + ch * kRowBytes + ((tg ^ twist(ch)) << 4);                                                        \
-    *reinterpret_cast<uint4*>(lds + to) = make_uint4(dequant<4, I>(x[0], wide, s2, z2), dequant<4, I>(x[1], wide, s2, z2),             \
-                                                     dequant<4, I>(x[2], wide, s2, z2), dequant<4, I>(x[3], wide, s2, z2));            \
+    const uint4 k = make_uint4(dequant<4, I>(x[0], wide, s2, z2), dequant<4, I>(x[1], wide, s2, z2),                       \
+                               dequant<4, I>(x[2], wide, s2, z2), dequant<4, I>(x[3], wide, s2, z2));                      \
+    *reinterpret_cast<uint4*>(lds + to) = k;                                                                               \
+    if constexpr (REST) {                                                                                                  \
+      const int e = first + 2 * I + odd;                                                                                   \
+      const bool used = ch < kD;                                                                                           \
+      *reinterpret_cast<uint4*>(lds + rest + e * kRowBytes + ((tg ^ twist(e)) << 4)) =                                     \
+          make_uint4(used ? dropped<I>(x[0], k.x, s2, z2) : 0, used ? dropped<I>(x[1], k.y, s2, z2) : 0,                   \
+                     used ? dropped<I>(x[2], k.z, s2, z2) : 0, used ? dropped<I>(x[3], k.w, s2, z2) : 0);                  \
+    }                                                                                                                      \
   }
-    MIXKVQ_CHANNEL(0) MIXKVQ_CHANNEL(1) MIXKVQ_CHANNEL(2) MIXKVQ_CHANNEL(3)
+    MIXKVQ_CHANNEL(0) MIXKVQ_CHANNEL(1)
 #undef MIXKVQ_CHANNEL
   }
   for (int u = tid; u < k16 * 8; u += 256) {      // fp16: eight tokens of two neighbouring entries
@@ -387,7 +465,7 @@ __device__ __forceinline__ void unpack_values(unsigned char* lds, int values, in
   }
 }
 
-template <class Counts>
+template <bool REST, class Counts>
 __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(ChunkArgs a, Counts counts) {
   __shared__ __align__(256) unsigned char lds[kLdsBytes];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -439,7 +517,9 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       const scalar_ptr table = (scalar_ptr)(uintptr_t)(a.table + (size_t)b * a.NB);
       return (const unsigned char*)a.blocks + (a.table ? (size_t)table[blk] * Hkv + j : (size_t)p * a.NB + blk) * a.rec_bytes;
     };
-    uint4 raw[3];      // this thread's 16-byte pieces of a tile on their way: pieces tid, tid + 512 and tid + 1024 of its records
+    constexpr int kPieces = REST ? 2 : 3;
+    uint4 raw[kPieces];      // this thread's 16-byte pieces of a tile on their way: pieces tid, tid + 512 .. of its records
+    static_assert(kOffRest - kOffRaw == 2 * 16 * kChunkThreads, "two pieces to a thread where there are rests");
     static_assert(kMaxRec <= 3 * 16 * kChunkThreads && kChunkRecords == 4, "three pieces to a thread; record_of");
     int listed[2];     // wavefront w: entries of record w's list
     auto record_of = [](int i, int pieces) { return (i >= pieces) + (i >= 2 * pieces) + (i >= 3 * pieces); };
@@ -450,13 +530,13 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       if (tile_rec == 1) {
         const uint4* at = reinterpret_cast<const uint4*>(mine);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) raw[k] = at[tid + kChunkThreads * k < pieces ? tid + kChunkThreads * k : 0];
+        for (int k = 0; k < kPieces; ++k) raw[k] = at[tid + kChunkThreads * k < pieces ? tid + kChunkThreads * k : 0];
       } else {
         const unsigned char* from[kChunkRecords];
 #pragma unroll
         for (int r = 0; r < kChunkRecords; ++r) from[r] = record(t * tile_rec + (r < cnt ? r : 0)) - r * a.rec_bytes;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {      // (pieces that the tile does not have: its first one once more)
+        for (int k = 0; k < kPieces; ++k) {      // (pieces that the tile does not have: its first one once more)
           const int i = tid + kChunkThreads * k < cnt * pieces ? tid + kChunkThreads * k : 0;
           const unsigned char* at = i < pieces ? from[0] : i < 2 * pieces ? from[1] : i < 3 * pieces ? from[2] : from[3];
           raw[k] = *reinterpret_cast<const uint4*>(at + i * 16);
@@ -471,7 +551,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       ArgsIn& a = args_here();
       const int cnt = tile_count(t), nvg_bits = a.nvg_bits, pieces = a.rec_bytes >> 4, plane = a.R * 2 << nvg_bits, tid = tid_here();
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
+      for (int k = 0; k < kPieces; ++k) {
         const int i = tid + kChunkThreads * k, rec = record_of(i, pieces), po = (i - rec * pieces) << 4;
         if (i >= cnt * pieces || (po >= a.off_v) != values) continue;
         const int es = po - a.off_v_s, ez = po - a.off_v_z;
@@ -513,13 +593,19 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
     };
 
     auto tokens_of = [&](int t) { return tile_count(t) * a.R; };
+    if constexpr (REST) {
+      *reinterpret_cast<uint4*>(lds + kOffRest + tid * 16) = make_uint4(0, 0, 0, 0);      // (rows behind the list stay 0)
+      if (tid < 72) *reinterpret_cast<_Float16*>(lds + kOffPick + tid * 2) = (_Float16)(tid / 8 == tid % 8 ? 1.f : 0.f);
+      static_assert(2 * kRestBytes == 16 * kChunkThreads, "a piece to a thread");
+    }
     fetch(t_first);
     list_channels(t_first);
     stage(t_first, false);
     stage(t_first, true);
     if (t_first + 1 < r_end) fetch(t_first + 1);
     __syncthreads();
-    if (wave < 4) unpack_keys(lds, 0, map_of(t_first), tokens_of(t_first));
+    unsigned entries = REST ? list_entries(lds, tile_count(t_first)) : 0, entries_next = entries;      // of this tile's lists and the next one's
+    if (wave < 4) unpack_keys<REST>(lds, 0, kOffRest, map_of(t_first), tokens_of(t_first));
     else unpack_values(lds, kKeyBytes, tokens_of(t_first));
     __syncthreads();
     if (t_first + 1 < r_end) {
@@ -527,19 +613,22 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       list_channels(t_first + 1);
     }
     Pipe<true> in;
-    if (active) begin<true>(lds, in, tokens_of(t_first), tokens_of(t_first), c, sc[0], pw[1], st);
+    if (active) begin<REST>(lds, in, entries, tokens_of(t_first), tokens_of(t_first), c, sc[0], pw[1], st);
     for (int t = t_first; t < r_end; ++t) {
       const bool next = t + 1 < r_end, next2 = t + 2 < r_end;
-      const int here = (t - t_first & 1) * kTileBytes, there = kTileBytes - here, n_tok = tokens_of(t), n_next = next ? tokens_of(t + 1) : 0;
+      const int odd = t - t_first & 1, here = odd * kTileBytes, there = kTileBytes - here;
+      const int rest_here = kOffRest + odd * kRestBytes, rest_there = kOffRest + kRestBytes - odd * kRestBytes;
+      const int n_tok = tokens_of(t), n_next = next ? tokens_of(t + 1) : 0;
       __syncthreads();      // this tile's values are there, and the next one's keys are staged
       if (next) stage(t + 1, true);
       if (next2) fetch(t + 2);
       // The wavefronts of a SIMD (w and w + 4) unpack at different times: one's vector instructions run beside the other's matrix
       // instructions.
-      if (next && wave < 4) unpack_keys(lds, there, map_of(t + 1), tokens_of(t + 1));
+      if (next && wave < 4) unpack_keys<REST>(lds, there, rest_there, map_of(t + 1), tokens_of(t + 1));
+      if (REST && next) entries_next = list_entries(lds, tile_count(t + 1));
       if (active) {
-        step<0>(lds, in, t == t_first ? 0 : here - there, sc[0], sc[1], pw[1], pw[0], 2 * 32 > n_tok, n_tok, c, st);
-        step<1>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 3 * 32 > n_tok, n_tok, c, st);
+        step<0, REST>(lds, in, t == t_first ? 0 : here - there, rest_here - here, entries, sc[0], sc[1], pw[1], pw[0], 2 * 32 > n_tok, n_tok, c, st);
+        step<1, REST>(lds, in, 0, rest_here - here, entries, sc[1], sc[0], pw[0], pw[1], 3 * 32 > n_tok, n_tok, c, st);
       }
       __syncthreads();      // the next tile's keys are there, and its values are staged
       if (next2) {
@@ -548,9 +637,10 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       }
       if (next && wave >= 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1));
       if (active) {         // (behind the last tile: scores of what the other tile's place holds, all of them hidden)
-        step<2>(lds, in, there - here, sc[0], sc[1], pw[1], pw[0], 4 * 32 > n_tok, n_tok, c, st);
-        step<3>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 32 > n_next, n_next, c, st);
+        step<2, REST>(lds, in, there - here, rest_here - here, entries, sc[0], sc[1], pw[1], pw[0], 4 * 32 > n_tok, n_tok, c, st);
+        step<3, REST>(lds, in, 0, rest_there - there, entries_next, sc[1], sc[0], pw[0], pw[1], 32 > n_next, n_next, c, st);
       }
+      entries = entries_next;
     }
     if (active) finish(lds, in, pw[1], st);
     __syncthreads();
@@ -592,7 +682,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
     // Tokens of the tile that a row sees, and those that all rows of the wavefront see.
     auto limit_of = [&](int t) { return (t < nt_rec + nt_win ? n_fp16 : token + 1) - first_of(t); };
     auto all_of = [&](int t) { return (t < nt_rec + nt_win ? n_fp16 : see_min) - first_of(t); };
-    if (active) begin<false>(lds, in, all_of(f_first), limit_of(f_first), c, sc[0], pw[1], st);
+    if (active) begin<false>(lds, in, 0u, all_of(f_first), limit_of(f_first), c, sc[0], pw[1], st);
     for (int t = f_first; t < t_end; ++t) {
       const bool next = t + 1 < t_end;
       const int here = (t - f_first & 1) * kTileBytes, there = kTileBytes - here;
@@ -600,8 +690,8 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       __syncthreads();      // this tile's values are there
       if (next) fetch(t + 1, true);
       if (active) {
-        step<0>(lds, in, t == f_first ? 0 : here - there, sc[0], sc[1], pw[1], pw[0], 2 * 32 > all, limit, c, st);
-        step<1>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 3 * 32 > all, limit, c, st);
+        step<0, false>(lds, in, t == f_first ? 0 : here - there, 0, 0u, sc[0], sc[1], pw[1], pw[0], 2 * 32 > all, limit, c, st);
+        step<1, false>(lds, in, 0, 0, 0u, sc[1], sc[0], pw[0], pw[1], 3 * 32 > all, limit, c, st);
       }
       if (next) {
         store(t + 1, there);
@@ -610,8 +700,8 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       __syncthreads();      // the next tile's keys are there
       if (active) {
         const int all_next = next ? all_of(t + 1) : 0, limit_next = next ? limit_of(t + 1) : 0;
-        step<2>(lds, in, there - here, sc[0], sc[1], pw[1], pw[0], 4 * 32 > all, limit, c, st);
-        step<3>(lds, in, 0, sc[1], sc[0], pw[0], pw[1], 32 > all_next, limit_next, c, st);
+        step<2, false>(lds, in, there - here, 0, 0u, sc[0], sc[1], pw[1], pw[0], 4 * 32 > all, limit, c, st);
+        step<3, false>(lds, in, 0, 0, 0u, sc[1], sc[0], pw[0], pw[1], 32 > all_next, limit_next, c, st);
       }
       if (next) store(t + 1, there + kKeyBytes);
     }
@@ -736,10 +826,16 @@ hipError_t start_chunk_few_1(const ChunkArgs& a, const ChunkCounts* c, int units
 hipError_t start_chunk_few_2(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
 hipError_t start_chunk_few_3(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s);
 
+// Rests of the 4-bit tier where a slice lies in one record, the list has at most 16 entries and records leave room for them.
+static bool has_rest(const ChunkArgs& a) { return a.k4 > 0 && a.k4 <= kRestRows && a.R % 32 == 0 && a.tile_rec * a.rec_bytes <= kOffRest - kOffRaw; }
+
 static hipError_t start_tiles(const ChunkArgs& a, const ChunkCounts* c, int units, hipStream_t s) {
   const dim3 grid(units * a.Hkv, a.row_tiles);
-  if (c) chunk_attention_kernel<ChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, *c);
-  else chunk_attention_kernel<NoChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, NoChunkCounts{});
+  const bool rest = has_rest(a);
+  if (c && rest) chunk_attention_kernel<true, ChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, *c);
+  else if (c) chunk_attention_kernel<false, ChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, *c);
+  else if (rest) chunk_attention_kernel<true, NoChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, NoChunkCounts{});
+  else chunk_attention_kernel<false, NoChunkCounts><<<grid, kChunkThreads, 0, s>>>(a, NoChunkCounts{});
   return hipGetLastError();
 }
 
