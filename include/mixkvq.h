@@ -254,9 +254,14 @@ int mixkvq_decode_step(mixkvq_cache* c, const void* k_new, const void* v_new, co
  *   workspace  DEVICE, on 16 bytes, at least mixkvq_chunk_workspace(c, n_new, n_seq) bytes for the cache's state at the call (NULL if
  *        that is 0), else ESCRATCH.  It needs no clearing and holds nothing between calls; calls that may overlap
  *        (two streams, two captured graphs) need one each.
- * Any cache state, configuration and storage layout; the sequences may differ in length whatever B is.  Precision:
- * dequantized keys and values and the weights of the softmax are rounded to binary16 (saturating) before the products, sums are
- * binary32; the bound of mixkvq_decode_attention holds. */
+ * Any cache state, configuration and storage layout; the sequences may differ in length whatever B is.  out and lse overlap none of
+ * the inputs.  Values that are not finite are outside the contract, in tokens that a row does not see as well.
+ * Precision: sums are binary32, the weights of the softmax and dequantized values are rounded to binary16 (saturating) before
+ * their product.  With few query rows per KV head the keys enter without a rounding of their own (the queries times their scales,
+ * to 22 bits, against the codes); with many each dequantized key is rounded to binary16, except that a 4-bit tier of up to 16
+ * channels in blocks of a multiple of 32 tokens keeps what that drops.  A score is then off by up to 2^-11 of the sum of |q k|
+ * over the other channels, which the bound of mixkvq_decode_attention covers for scores of ordinary size but not for sharp
+ * softmaxes over scores in the tens.  Which of the two forms a call takes depends on its sizes alone. */
 int64_t mixkvq_chunk_workspace(const mixkvq_cache* c, int32_t n_new, const int32_t* n_seq);   /* bytes, or a negative code */
 int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strides[3], const void* k_new, const void* v_new,
                            const int64_t kv_strides[3], int32_t n_new, const int32_t* n_seq, void* out,
