@@ -254,7 +254,8 @@ int mixkvq_decode_step(mixkvq_cache* c, const void* k_new, const void* v_new, co
  *   workspace  DEVICE, on 16 bytes, at least mixkvq_chunk_workspace(c, n_new, n_seq) bytes for the cache's state at the call (NULL if
  *        that is 0), else ESCRATCH.  It needs no clearing and holds nothing between calls; calls that may overlap
  *        (two streams, two captured graphs) need one each.
- * Any cache state, configuration and storage layout; the sequences may differ in length whatever B is.  out and lse overlap none of
+ * Any cache state, configuration and storage layout; the sequences may differ in length whatever B is.  The counts, the cache's and
+ * n_seq's, are those of the call: a captured call replays with the counts of its capture.  out and lse overlap none of
  * the inputs.  Values that are not finite are outside the contract, in tokens that a row does not see as well.
  * Precision: sums are binary32, the weights of the softmax and dequantized values are rounded to binary16 (saturating) before
  * their product.  With few query rows per KV head the keys enter without a rounding of their own (the queries times their scales,
@@ -282,7 +283,8 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
  *   u_accept  DEVICE fp32 [B][n_draft], u_next DEVICE fp32 [B]: uniform in [0, 1).
  *   n_accepted DEVICE int32 [B];  tokens DEVICE int32 [B][n_draft + 1]: the drafts that stay, the next token, then -1.
  *   workspace DEVICE, on 16 bytes, mixkvq_verify_workspace(B, V) bytes (else ESCRATCH); one for every call that may overlap.
- * n_draft <= 64 (0: draws from p_target); draft and u_accept may be NULL if it is 0.  Needs no cache. */
+ * n_draft <= 64 (0: draws from p_target), V <= 2^30; draft and u_accept may be NULL if n_draft is 0.  Pointers are on the 4 bytes of
+ * their elements.  Needs no cache. */
 int64_t mixkvq_verify_workspace(int32_t B, int32_t V);   /* bytes, or a negative code */
 int mixkvq_verify_draft(int32_t B, int32_t n_draft, int32_t V, const float* p_target, const int64_t p_target_strides[2],
                         const float* p_draft, const int64_t p_draft_strides[2], const int32_t* draft, const int32_t* n_seq,

@@ -12,6 +12,7 @@ namespace mixkvq {
 
 constexpr int kVerifyThreads = 256, kPickThreads = 1024;
 constexpr int kVerifyMaxSpans = 64;
+constexpr int kVerifyMaxV = 1 << 30;     // (token numbers behind a row's end stay 32-bit)
 constexpr int kParts = kVerifyThreads / 64;      // of a span, one to a wavefront
 constexpr int kVerifyMaxDraft = 64;      // a wavefront forms the verdict
 
@@ -277,7 +278,7 @@ using namespace mixkvq;
 extern "C" {
 
 int64_t mixkvq_verify_workspace(int32_t B, int32_t V) {
-  if (B < 1 || B > (1 << 20) || V < 1) return MIXKVQ_EINVAL;
+  if (B < 1 || B > (1 << 20) || V < 1 || V > kVerifyMaxV) return MIXKVQ_EINVAL;
   return (int64_t)B * verify_spans(B, V) * kParts * (int64_t)sizeof(double2);
 }
 
@@ -285,10 +286,12 @@ int mixkvq_verify_draft(int32_t B, int32_t n_draft, int32_t V, const float* p_ta
                         const float* p_draft, const int64_t p_draft_strides[2], const int32_t* draft, const int32_t* n_seq,
                         const float* u_accept, const float* u_next, int32_t* n_accepted, int32_t* tokens, void* workspace,
                         int64_t workspace_bytes, void* stream) {
-  if (B < 1 || B > (1 << 20) || V < 1 || n_draft < 0 || n_draft > kVerifyMaxDraft) return MIXKVQ_EINVAL;
+  if (B < 1 || B > (1 << 20) || V < 1 || V > kVerifyMaxV || n_draft < 0 || n_draft > kVerifyMaxDraft) return MIXKVQ_EINVAL;
   if (!p_target || !p_target_strides || !u_next || !n_accepted || !tokens) return MIXKVQ_EINVAL;
   if (n_draft > 0 && (!draft || !u_accept)) return MIXKVQ_EINVAL;
   if (p_draft && !p_draft_strides) return MIXKVQ_EINVAL;
+  for (const void* x : {(const void*)p_target, (const void*)p_draft, (const void*)draft, (const void*)n_seq, (const void*)u_accept, (const void*)u_next, (const void*)n_accepted, (const void*)tokens})
+    if ((uintptr_t)x & 3u) return MIXKVQ_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 15u)) return MIXKVQ_EINVAL;
   VerifyArgs a{};
   a.spans = verify_spans(B, V);

@@ -89,6 +89,8 @@ def _verify(M, **change):
 @pytest.mark.parametrize("change", [
     dict(B=0), dict(B=(1 << 20) + 1), dict(V=0), dict(V=-5), dict(n=-1), dict(n=65), dict(p=None), dict(ps=None), dict(qs=None), dict(draft=None),
     dict(u=None), dict(u_next=None), dict(accepted=None), dict(tokens=None), dict(workspace=None), dict(workspace=AT + 8),
+    dict(V=(1 << 30) + 1), dict(p=AT + 2), dict(q=AT + 1), dict(draft=AT + 2), dict(n_seq=AT + 1), dict(u=AT + 2), dict(u_next=AT + 3),
+    dict(accepted=AT + 2), dict(tokens=AT + 1),
 ])
 def test_verify_draft_refuses(M, change):
     assert _verify(M, **change) == EINVAL
@@ -96,7 +98,7 @@ def test_verify_draft_refuses(M, change):
 
 def test_verify_workspace(M):
     lib = M.load_library()
-    for bad in ((0, 10), ((1 << 20) + 1, 10), (4, 0)):
+    for bad in ((0, 10), ((1 << 20) + 1, 10), (4, 0), (1, (1 << 30) + 1)):
         assert lib.mixkvq_verify_workspace(*bad) == EINVAL
     for B, V in ((1, 1), (2, 50000), (128, 50000), (64, 152064), (1, 1 << 30)):
         need = lib.mixkvq_verify_workspace(B, V)
