@@ -32,19 +32,20 @@ static int splits_of(int steps, int chain) {
   return s > kChunkMaxSplits ? kChunkMaxSplits : s;
 }
 
-// The cut of a call for one kernel that takes the least time, and that time in microseconds.  A unit (one split of one tile of
-// rows) costs its steps and a constant part.  Workgroups of one length run in rounds; of several (later rows of a chunk see more
-// tokens, and the longest start first) they fill the compute units evenly until the shortest ones end.  Splits have to be merged,
-// which costs a launch and their rows' traffic.  The constants fit what was measured for cuts of 1 to 258 steps, e.g. few rows
-// (8 sequences of 32k): 17 steps a unit 69 us, 9 steps 88, 19 steps 73; tiles (1000 after 31000 tokens): 28 steps 653 us,
-// 14 steps 742, 126 steps 678; (8192 tokens, empty cache): unsplit 508 us, 32 steps 595.
+// The cut of a call for one kernel and tile of rows that takes the least time, and that time in microseconds.  A unit (one split of
+// one tile of rows) costs its steps and a constant part.  Workgroups of one length run in rounds; of several (later rows of a
+// chunk see more tokens, and the longest start first) they fill the compute units evenly until the shortest ones end.  Splits have
+// to be merged, which costs a launch and their rows' traffic.  The constants fit what was measured for cuts of 1 to 258 steps, e.g.
+// 48 rows (8 sequences of 32k): 17 steps a unit 66 us, 9 steps 83, 19 steps 69; 16 rows (one of 32k): 9 steps 28 us, 5 steps 39;
+// tiles (1000 after 31000 tokens): 28 steps 653 us, 14 steps 742, 126 steps 678; (8192 tokens, empty cache): unsplit 508 us, 32 steps 595.
 static double cut_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq, ChunkPlan* pl) {
   static const int kTry[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64};
   constexpr int kTries = sizeof kTry / sizeof kTry[0];
   static_assert(kChunkMaxSplits == 64, "the last try");
   const mixkvq_config& cfg = c->v.cfg;
-  const int fixed = pl->few ? 6 : 2;
-  const double step_us = pl->few ? 2.5 : 4.8;
+  const double more = (c->v.lay.NVG > 1 ? 0.7 : 0) + (cfg.k16 ? 0.25 : 0);      // values dequantized one by one, the fp16 tier
+  const double step_us = !pl->few ? 4.8 : more + (pl->rows == 16 ? 1.15 : pl->rows == 32 ? 1.65 : 2.1);
+  const double fixed_us = !pl->few ? 10 : pl->rows == 16 ? 12 : pl->rows == 32 ? 16 : 22, merge_us = pl->few ? 6 : 10;
   int longest = 1, shortest = 1 << 30, chain[kTries];
   bool equal = true;      // (the longest start first only among a sequence's own row tiles)
   int64_t units[kTries] = {};
@@ -75,11 +76,11 @@ static double cut_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq, 
   }
   double best = 0;
   for (int i = 0; i < kTries && kTry[i] <= longest; ++i) {
-    const double rounds = (double)((units[i] + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain[i] + fixed);
-    const double even = (steps + (double)fixed * units[i]) / kChunkUnitsAtOnce + (equal && shortest < chain[i] ? shortest : chain[i]) + fixed;
+    const double rounds = (double)((units[i] + kChunkUnitsAtOnce - 1) / kChunkUnitsAtOnce) * (chain[i] * step_us + fixed_us);
+    const double even = (steps * step_us + fixed_us * units[i]) / kChunkUnitsAtOnce + (equal && shortest < chain[i] ? shortest : chain[i]) * step_us + fixed_us;
     // (rounds are exact if there is one; of units of one length they are a bound from above, else hopeful)
     const bool less = units[i] <= kChunkUnitsAtOnce || (equal ? rounds < even : rounds > even);
-    const double t = ((less ? rounds : even) + (i ? 2 + units[i] * pl->rows / 32768.0 : 0)) * step_us;
+    const double t = (less ? rounds : even) + (i ? merge_us + units[i] * pl->rows / 7000.0 : 0);
     if (i == 0 || t < best) {
       best = t;
       pl->chain = chain[i];
@@ -89,21 +90,26 @@ static double cut_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq, 
 }
 
 // The kernel for few rows reads every record anew for each 16, 32 or 48 of them, the one with tiles of 256 rows dequantizes it once in
-// LDS.  Where the second starts to win depends on the compute units that each leaves idle: 24 sequences of 8k tokens, 161
-// rows, 297 and 195 us; 8 of 16k, 161 rows, 106 and 118 us, 196 rows, 148 and 121 us; one of 32k, 259 rows, 58 and 78 us.
+// LDS.  Tiles of 16 rows are the quickest ones where they leave compute units idle (35 rows: a window of 90 tokens 7.0, 9.4 and 11.1 us,
+// 3000 tokens 16.7, 19.8 and 22.9, 32805 tokens 27.6, 32.5 and 38.7), of 48 where they do not (8 sequences of 32805: 82, 77 and 66 us).
+// Where the tiles of 256 start to win depends on that as well: 24 sequences of 8k tokens, 161 rows, 297 and 195 us; 8 of 16k, 161
+// rows, 106 and 118 us, 196 rows, 148 and 121 us; one of 32k, 259 rows, 58 and 78 us.
 static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
   int most = 0;
   for (int b = 0; b < c->v.cfg.B; ++b) most = n_new_of(n_seq, n_max, b) > most ? n_new_of(n_seq, n_max, b) : most;
   const int rows = most * c->v.g;
-  ChunkPlan tiles{false, 256, 1}, few{true, rows <= 16 ? 16 : rows <= 32 || chunk_few_rows(c->v) == 32 ? 32 : 48, 1};
+  ChunkPlan best{false, 256, 1};
   const bool fits = chunk_few_fits(c->v);
-  if (!fits || rows > kFewRows) {
-    cut_chunk(c, n_max, n_seq, &tiles);
-    return tiles;
+  double us = rows > 48 || !fits ? cut_chunk(c, n_max, n_seq, &best) : 0;
+  for (int r = 16; fits && rows <= kFewRows && r <= chunk_few_rows(c->v) && r - 16 < rows; r += 16) {
+    ChunkPlan few{true, r, 1};
+    const double t = cut_chunk(c, n_max, n_seq, &few);
+    if (us == 0 || t < us) {
+      us = t;
+      best = few;
+    }
   }
-  const double few_us = cut_chunk(c, n_max, n_seq, &few);
-  if (rows <= 48) return few;
-  return few_us <= cut_chunk(c, n_max, n_seq, &tiles) ? few : tiles;
+  return best;
 }
 
 // Sequences [b0, b0 + n) of the call as one launch (counts that differ in *c).  How many sequences a launch takes is up to the

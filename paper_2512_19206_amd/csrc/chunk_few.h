@@ -245,6 +245,24 @@ struct Kernel {
       load_words(rec, sl, val);
     }
 
+    // Keys of slice u of the fp16 rows: the lane's tokens and channels as the first product takes them.  Where they come first they are
+    // asked for before q as well (with more rows there are no registers for that).
+    uint4 kr[2][4];
+    auto load_fp16_keys = [&](int u) __attribute__((always_inline)) {
+      const bool win = u < u_rec + u_win;
+      const int first = (u - u_rec - (win ? 0 : u_win)) * 32, n = win ? n_fp16 : seen;
+      const __half* k = win ? a.res_k + (size_t)p * a.RW * kD : a.k + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
+      const int step = win ? kD : (int)a.kvs.t;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        int r = first + tok0 + 4 * t;
+        r = r < n ? r : n - 1;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) kr[t][s] = *reinterpret_cast<const uint4*>(k + (int64_t)r * step + 32 * s + 8 * grp);
+      }
+    };
+    if (NB == 1 && !records && u0 < u1) load_fp16_keys(u0);
+
     // ---- the rows of q, each brought to a largest element of 2^6 to 2^7 (powers of two: exact) ----
     float* const row_scale = reinterpret_cast<float*>(lds + kOffScale);
 #pragma unroll 1
@@ -535,17 +553,10 @@ struct Kernel {
     for (int u = u0 > u_rec ? u0 : u_rec; u < u1; ++u) {
       const bool win = u < u_rec + u_win;
       const int first = (u - u_rec - (win ? 0 : u_win)) * 32, n = win ? n_fp16 : seen;
-      const __half* k = win ? a.res_k + (size_t)p * a.RW * kD : a.k + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
       const __half* v = win ? a.res_v + (size_t)p * a.RW * kD : a.v + (int64_t)b * a.kvs.b + (int64_t)j * a.kvs.h;
       const int step = win ? kD : (int)a.kvs.t;
-      uint4 kr[2][4], vr[8];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        int r = first + tok0 + 4 * t;
-        r = r < n ? r : n - 1;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) kr[t][s] = *reinterpret_cast<const uint4*>(k + (int64_t)r * step + 32 * s + 8 * grp);
-      }
+      uint4 vr[8];
+      if (NB > 1 || records || u > u0) load_fp16_keys(u);
       auto load_values = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
