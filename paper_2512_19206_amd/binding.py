@@ -8,6 +8,7 @@ not been built.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -123,7 +124,7 @@ class _on:
 
     def __init__(self, device, stream):
         self.ctx = []
-        if torch.cuda.current_device() != (device.index or 0):
+        if (_device() if _device else torch.cuda.current_device()) != (device.index or 0):
             self.ctx.append(torch.cuda.device(device))
         if stream is not None:
             self.ctx.append(torch.cuda.stream(stream))
@@ -143,12 +144,23 @@ _I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
 def _strides3(t: torch.Tensor):
     st = t.stride()
     assert len(st) == 4 and st[3] == 1, "expected [B, H, L, D] with unit channel stride"
-    return _I64x3(st[0], st[1], st[2])
+    return _i64x3(st[0], st[1], st[2])
 
 
 def _strides2(t: torch.Tensor):
     st = t.stride()
-    return _I64x2(st[0], st[1])
+    return _i64x2(st[0], st[1])
+
+
+# Arrays of three and two numbers, which the library only reads: making one takes 0.3 us of a 10 us call.
+@functools.lru_cache(maxsize=1024)
+def _i64x3(a, b, c):
+    return _I64x3(a, b, c)
+
+
+@functools.lru_cache(maxsize=1024)
+def _i64x2(a, b):
+    return _I64x2(a, b)
 
 
 def make_config(**kw) -> Config:
@@ -189,6 +201,7 @@ class Cache:
         h = C.c_void_p()
         _check(self.lib.mixkvq_cache_create(C.byref(cfg), C.byref(bufs), C.byref(h)))
         self.handle = h
+        self._known = (cfg.B, cfg.Hq, cfg.Hkv, cfg.D, torch.bfloat16 if cfg.in_dtype else torch.float16, self.device.index or 0)
         self.reset()
 
     def __del__(self):
@@ -352,12 +365,10 @@ class Cache:
         multiples of 8).  n_seq: new tokens of each sequence (host integers) or None.  Attention of the n new tokens over the
         cache and, causally, over themselves; nothing is appended.  Returns (out [B, Hq, n, D], strides as q's unless given, and
         lse fp32 [B, Hq, n]); rows behind a sequence's n_seq are left as they are."""
-        B, Hq, n, D = q.shape
-        cfg = self.cfg
-        assert (B, Hq, D) == (cfg.B, cfg.Hq, cfg.D) and k_new.shape == (B, cfg.Hkv, n, D) == v_new.shape
-        dt = torch.bfloat16 if cfg.in_dtype else torch.float16
+        B, Hq, n, D = shape = q.shape
+        B_, Hq_, Hkv, D_, dt, at = self._known
+        assert B == B_ and Hq == Hq_ and D == D_ and k_new.shape == (B, Hkv, n, D) == v_new.shape
         assert k_new.stride() == v_new.stride() and q.dtype == k_new.dtype == v_new.dtype == dt
-        at = self.device.index or 0
         assert q.get_device() == k_new.get_device() == v_new.get_device() == at
         counts = None
         if n_seq is not None:
@@ -367,18 +378,20 @@ class Cache:
             if out is None:
                 out = torch.empty_like(q)
             if lse is None:
-                lse = torch.empty((B, Hq, n), dtype=torch.float32, device=self.device)
-            assert out.shape == q.shape and out.dtype == dt and out.get_device() == at
-            assert lse.shape == (B, Hq, n) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == at
-            need = self.lib.mixkvq_chunk_workspace(self.handle, n, counts)
-            _check(min(need, 0))
-            if workspace is None and need:
-                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+                lse = q.new_empty((B, Hq, n), dtype=torch.float32)
+            else:
+                assert lse.shape == (B, Hq, n) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == at
+            assert out.shape == shape and out.dtype == dt and out.get_device() == at
+            if workspace is None:
+                need = self.lib.mixkvq_chunk_workspace(self.handle, n, counts)
+                if need:
+                    _check(min(need, 0))
+                    workspace = q.new_empty(need, dtype=torch.uint8)
             assert workspace is None or (workspace.get_device() == at and workspace.is_contiguous())
             wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
             _check(self.lib.mixkvq_chunk_attention(self.handle, q.data_ptr(), _strides3(q), k_new.data_ptr(), v_new.data_ptr(),
                                                    _strides3(k_new), n, counts, out.data_ptr(), _strides3(out), lse.data_ptr(),
-                                                   float(scale), int(bool(accumulate_q)), wp, wn, _stream_ptr(stream)))
+                                                   scale, bool(accumulate_q), wp, wn, _stream_ptr(stream)))
         return out, lse
 
     def set_timing_events(self, start_event, stop_event):
@@ -436,23 +449,25 @@ def verify_draft(p_target, draft, u_accept, u_next, p_draft=None, n_seq=None, n_
         assert n_seq.shape == (B,) and n_seq.dtype == torch.int32 and n_seq.is_contiguous()
     device, at = p_target.device, p_target.get_device()
     assert at == draft.get_device() == u_accept.get_device() == u_next.get_device()
-    assert all(t is None or t.get_device() == at for t in (p_draft, n_seq, n_accepted, tokens, workspace))
+    for t in (p_draft, n_seq, n_accepted, tokens, workspace):
+        assert t is None or t.get_device() == at
     with _on(device, stream):
         if n_accepted is None:
-            n_accepted = torch.empty(B, dtype=torch.int32, device=device)
+            n_accepted = draft.new_empty(B)
+        else:
+            assert n_accepted.shape == (B,) and n_accepted.dtype == torch.int32 and n_accepted.is_contiguous()
         if tokens is None:
-            tokens = torch.empty((B, n1), dtype=torch.int32, device=device)
-        assert n_accepted.shape == (B,) and n_accepted.dtype == torch.int32 and n_accepted.is_contiguous()
-        assert tokens.shape == (B, n1) and tokens.dtype == torch.int32 and tokens.is_contiguous()
-        need = lib.mixkvq_verify_workspace(B, V)
-        _check(min(need, 0))
+            tokens = draft.new_empty((B, n1))
+        else:
+            assert tokens.shape == (B, n1) and tokens.dtype == torch.int32 and tokens.is_contiguous()
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            need = lib.mixkvq_verify_workspace(B, V)
+            _check(min(need, 0))
+            workspace = draft.new_empty(need, dtype=torch.uint8)
         assert workspace.is_contiguous()
-        _check(lib.mixkvq_verify_draft(B, n, V, p_target.data_ptr(), _I64x2(p_target.stride(0), p_target.stride(1)),
-                                       None if p_draft is None else p_draft.data_ptr(),
-                                       None if p_draft is None else _I64x2(p_draft.stride(0), p_draft.stride(1)),
-                                       draft.data_ptr(), None if n_seq is None else n_seq.data_ptr(), u_accept.data_ptr(),
-                                       u_next.data_ptr(), n_accepted.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
+        pd, ps = (None, None) if p_draft is None else (p_draft.data_ptr(), _strides2(p_draft))
+        _check(lib.mixkvq_verify_draft(B, n, V, p_target.data_ptr(), _strides2(p_target), pd, ps, draft.data_ptr(),
+                                       None if n_seq is None else n_seq.data_ptr(), u_accept.data_ptr(), u_next.data_ptr(),
+                                       n_accepted.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
     return n_accepted, tokens
