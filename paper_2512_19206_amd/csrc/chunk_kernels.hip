@@ -353,15 +353,12 @@ __device__ __forceinline__ void finish(unsigned char* lds, Pipe<BY_CHANNEL>& in,
   }
 }
 
-// Dequantizes the staged tile's keys into `keys` (a row per channel).  Threads 0 .. 255; threads 256 .. 511 do the values.
-// REST: and what binary16 drops of the 4-bit tier into `rest` (a row per list entry).
-template <bool REST>
-__device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, int rest, const unsigned short* map, int n_tok) {
+// Dequantizes the 2-bit channels of the staged tile's keys into `keys` (a row per channel): threads 0 .. 255.
+__device__ __forceinline__ void unpack_low_keys(unsigned char* lds, int keys, const unsigned short* map, int n_tok) {
   ArgsIn& a = args_here();
   const int Rr = a.R, inv_r = a.inv_r, inv_gk = a.inv_gk, tid = tid_here();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const unsigned two[5] = {in_vgpr(CodeAt<2, 0>::kMask), in_vgpr(CodeAt<2, 1>::kMask), in_vgpr(CodeAt<2, 2>::kMask), in_vgpr(CodeAt<2, 3>::kMask), in_vgpr(CodeAt<2, 4>::kMask)};
-  const unsigned wide[5] = {in_vgpr(CodeAt<4, 0>::kMask), in_vgpr(CodeAt<4, 1>::kMask), 0, 0, 0};
   {  // 2-bit channels: eight tokens of the eight even or odd channels of a word
     const int odd = wave & 1, tg = (wave >> 1) * 8 + (lane & 7), w = lane >> 3, t = tg * 8;
     if (w < a.Wlo && t < n_tok) {
@@ -390,9 +387,17 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, int re
 #undef MIXKVQ_CHANNEL
     }
   }
-  // Side tiers: their channels stand in the record's list, an unused entry (255) goes to the row that nobody reads.
+}
+
+// The other tiers, whose channels stand in the record's list (an unused entry, 255, goes to the row that nobody reads): threads
+// 256 .. 511.  REST: and what binary16 drops of the 4-bit tier into `rest` (a row per list entry).
+template <bool REST>
+__device__ __forceinline__ void unpack_side_keys(unsigned char* lds, int keys, int rest, int n_tok) {
+  ArgsIn& a = args_here();
+  const int Rr = a.R, inv_r = a.inv_r, inv_gk = a.inv_gk, tid = tid_here() - 256;
+  const unsigned wide[5] = {in_vgpr(CodeAt<4, 0>::kMask), in_vgpr(CodeAt<4, 1>::kMask), 0, 0, 0};
   const int k4 = a.k4, k16 = a.k16;
-  for (int u = tid ^ 128; u < a.W4 * 64; u += 256) {      // four bits: eight tokens of two even or odd channels of a word
+  for (int u = tid; u < a.W4 * 64; u += 256) {      // four bits: eight tokens of two even or odd channels of a word
     const int odd = u & 1, late = (u >> 1) & 1, tg = (u >> 2) & 15, w = u >> 6, t = tg * 8;
     if (t >= n_tok) continue;
     const int rec = t * inv_r >> 16, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
@@ -426,7 +431,7 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, int re
     MIXKVQ_CHANNEL(0) MIXKVQ_CHANNEL(1)
 #undef MIXKVQ_CHANNEL
   }
-  for (int u = tid; u < k16 * 8; u += 256) {      // fp16: eight tokens of two neighbouring entries
+  for (int u = tid ^ 128; u < k16 * 8; u += 256) {      // fp16: eight tokens of two neighbouring entries
     const int tg = u & 15, e = (u >> 4) * 2, t = tg * 8;
     if (t >= n_tok) continue;
     const int rec = t * inv_r >> 16, tin = t - rec * Rr, raw = kOffRaw + rec * a.rec_bytes;
@@ -445,16 +450,17 @@ __device__ __forceinline__ void unpack_keys(unsigned char* lds, int keys, int re
   }
 }
 
-// The staged tile's values into `values` (a row per channel): threads 256 .. 511, a word of 16 tokens of one channel at a time.
+// Quarters from .. to - 1 of the staged tile's values into `values` (a row per channel), by 256 threads, a word of 16 tokens of one channel
+// at a time.
 // Places of tokens that the tile does not have become 0 (their weights are 0, and 0 times what the LDS held may be NaN).
-__device__ __forceinline__ void unpack_values(unsigned char* lds, int values, int n_tok) {
+__device__ __forceinline__ void unpack_values(unsigned char* lds, int values, int n_tok, int from, int to) {
   ArgsIn& a = args_here();
-  const int tid = tid_here() - 256, ch = tid & (kD - 1), first = __builtin_amdgcn_readfirstlane(tid >> 7);
+  const int tid = tid_here() & 255, ch = tid & (kD - 1), first = __builtin_amdgcn_readfirstlane(tid >> 7);
   const unsigned two[5] = {in_vgpr(CodeAt<2, 0>::kMask), in_vgpr(CodeAt<2, 1>::kMask), in_vgpr(CodeAt<2, 2>::kMask), in_vgpr(CodeAt<2, 3>::kMask), in_vgpr(CodeAt<2, 4>::kMask)};
   const int per = a.R >> 4;      // words of a record and channel
   const int vg = ch >> (7 - a.nvg_bits), row = values + ch * kRowBytes, tw = twist(ch);
 #pragma unroll 2
-  for (int k = 0; k < 4; ++k) {
+  for (int k = from; k < to; ++k) {
     const int w = first + 2 * k;
     uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
     int t0 = 16 * w, t1 = t0 + 8;
@@ -540,11 +546,12 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
     auto fetch = [&](int t) __attribute__((always_inline)) {
       ArgsIn& a = args_here();
       const int cnt = tile_count(t), pieces = a.rec_bytes >> 4, tid = tid_here();
-      const unsigned char* mine = record(t * tile_rec + (wave < cnt ? wave : 0));      // wavefront w: record w
-      if (tile_rec == 1) {
+      const unsigned char* mine = record(t * tile_rec);      // wavefront w < cnt lists record w
+      if (tile_rec == 1 || !a.table) {                       // one after the other
         const uint4* at = reinterpret_cast<const uint4*>(mine);
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) raw[k] = at[tid + kChunkThreads * k < pieces ? tid + kChunkThreads * k : 0];
+        for (int k = 0; k < kPieces; ++k) raw[k] = at[tid + kChunkThreads * k < cnt * pieces ? tid + kChunkThreads * k : 0];
+        mine += (wave < cnt ? wave : 0) * a.rec_bytes;
       } else {
         const unsigned char* from[kChunkRecords];
 #pragma unroll
@@ -555,6 +562,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
           const unsigned char* at = i < pieces ? from[0] : i < 2 * pieces ? from[1] : i < 3 * pieces ? from[2] : from[3];
           raw[k] = *reinterpret_cast<const uint4*>(at + i * 16);
         }
+        mine = record(t * tile_rec + (wave < cnt ? wave : 0));
       }
       const int ks = a.k4 + a.k16, lane = tid & 63;
       listed[0] = mine[a.off_idx + (lane < ks ? lane : 0)];
@@ -580,6 +588,12 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
           }
           unsigned short* to = reinterpret_cast<unsigned short*>(lds + kOffScale) + (scale ? 0 : 8 * kScaleRow) + rec * a.R;
           const unsigned v[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+          if (nvg_bits == 2) {      // two tokens of four groups
+#pragma unroll
+            for (int vg = 0; vg < 4; ++vg)
+              *reinterpret_cast<unsigned*>(to + vg * kScaleRow + (li >> 2)) = __builtin_amdgcn_perm(v[2 + (vg >> 1)], v[vg >> 1], vg & 1 ? 0x07060302u : 0x05040100u);
+            continue;
+          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const int tok = (li + e) >> nvg_bits, vg = (li + e) & ((1 << nvg_bits) - 1);
@@ -619,13 +633,15 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
     if (t_first + 1 < r_end) fetch(t_first + 1);
     __syncthreads();
     unsigned entries = REST ? list_entries(lds, tile_count(t_first)) : 0, entries_next = entries;      // of this tile's lists and the next one's
-    if (wave < 4) unpack_keys<REST>(lds, 0, kOffRest, map_of(t_first), tokens_of(t_first));
-    else unpack_values(lds, kKeyBytes, tokens_of(t_first));
+    if (wave < 4) unpack_low_keys(lds, 0, map_of(t_first), tokens_of(t_first));
+    else unpack_side_keys<REST>(lds, 0, kOffRest, tokens_of(t_first));
+    unpack_values(lds, kKeyBytes, tokens_of(t_first), wave < 4 ? 0 : 2, wave < 4 ? 2 : 4);
     __syncthreads();
     if (t_first + 1 < r_end) {
       stage(t_first + 1, false);
       list_channels(t_first + 1);
     }
+    const int share = n_rows - rt * kRows > kRows / 2;      // quarters of the values that wavefronts 0 .. 3 unpack: none where the others have no rows
     Pipe<true> in;
     if (active) begin<REST>(lds, in, entries, tokens_of(t_first), tokens_of(t_first), c, sc[0], pw[1], st);
     for (int t = t_first; t < r_end; ++t) {
@@ -638,22 +654,24 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       if (next2) fetch(t + 2);
       // The wavefronts of a SIMD (w and w + 4) unpack at different times: one's vector instructions run beside the other's matrix
       // instructions.
-      if (next && wave < 4) unpack_keys<REST>(lds, there, rest_there, map_of(t + 1), tokens_of(t + 1));
+      if (next && wave < 4) unpack_low_keys(lds, there, map_of(t + 1), tokens_of(t + 1));
       if (REST && next) entries_next = list_entries(lds, tile_count(t + 1));
       if (active) {
         step<0, REST>(lds, in, t == t_first ? 0 : here - there, rest_here - here, entries, sc[0], sc[1], pw[1], pw[0], 2 * 32 > n_tok, n_tok, c, st);
         step<1, REST>(lds, in, 0, rest_here - here, entries, sc[1], sc[0], pw[0], pw[1], 3 * 32 > n_tok, n_tok, c, st);
       }
+      if (next && wave >= 4) unpack_side_keys<REST>(lds, there, rest_there, tokens_of(t + 1));
       __syncthreads();      // the next tile's keys are there, and its values are staged
       if (next2) {
         stage(t + 2, false);
         list_channels(t + 2);
       }
-      if (next && wave >= 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1));
+      if (next && wave >= 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1), share, 4);
       if (active) {         // (behind the last tile: scores of what the other tile's place holds, all of them hidden)
         step<2, REST>(lds, in, there - here, rest_here - here, entries, sc[0], sc[1], pw[1], pw[0], 4 * 32 > n_tok, n_tok, c, st);
         step<3, REST>(lds, in, 0, rest_there - there, entries_next, sc[1], sc[0], pw[0], pw[1], 32 > n_next, n_next, c, st);
       }
+      if (next && wave < 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1), 0, share);
       entries = entries_next;
     }
     if (active) finish(lds, in, pw[1], st);
