@@ -8,7 +8,7 @@
 // one exchange between the two halves of the wavefront, and the weights P go into the second product from the registers in
 // which the first one left them.
 //
-// 256 rows, because a tile is dequantized once for all of them: unpacking takes 2 400 of a wavefront's 14 000 cycles for a tile of
+// 256 rows, because a tile is dequantized once for all of them: unpacking takes 3 500 of a wavefront's 13 000 cycles for a tile of
 // records.  Keys and values stand in LDS as binary16, two tiles of each (162 KB with the record on its way): the next tile is
 // unpacked while this one is used, its keys in the first half of the steps, its values in the second.  A wavefront keeps its 32
 // rows of Q and O in registers.
@@ -20,7 +20,8 @@
 // in turn, 8192 new tokens over an empty cache (28 query and 4 KV heads) took 645 and 581 us, and 497 us this way (967 TFLOP/s;
 // a large library product reaches 1 171 on this card).  Barriers (two to a tile), the tile's way through LDS and the start and end
 // of a workgroup take a third of the time.
-// 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 690 us, 655 TFLOP/s.
+// 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 685 us, 660 TFLOP/s; 2 x 2048 after
+// 8190 (records of 32) 1119 us, 691 TFLOP/s.
 #include <type_traits>
 #include "chunk.h"
 
