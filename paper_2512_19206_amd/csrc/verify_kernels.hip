@@ -10,7 +10,7 @@
 
 namespace mixkvq {
 
-constexpr int kVerifyThreads = 256, kPickThreads = 1024;
+constexpr int kVerifyThreads = 256, kAloneThreads = 1024;
 constexpr int kVerifyMaxSpans = 64;
 constexpr int kVerifyMaxV = 1 << 30;     // (token numbers behind a row's end stay 32-bit)
 constexpr int kParts = kVerifyThreads / 64;      // of a span, one to a wavefront
@@ -139,13 +139,14 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sum_kernel(VerifyArgs a
 }
 
 // ALONE: the only launch, its sixteen wavefronts form the sums of sixteen parts first.
-template <bool ALONE>
-__global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a) {
+template <bool ALONE, int kThreads>
+__global__ void __launch_bounds__(kThreads) verify_pick_kernel(VerifyArgs a) {
+  static_assert(!ALONE || kThreads == kAloneThreads, "sixteen parts");
   __shared__ double sBefore;
-  __shared__ double sWave[kPickThreads / 64];
+  __shared__ double sWave[kThreads / 64];
   __shared__ int sPart, sByRest, sFirst, sLast;
   __shared__ double sPoint;
-  __shared__ double2 sSums[ALONE ? kPickThreads / 64 : 1];
+  __shared__ double2 sSums[ALONE ? kThreads / 64 : 1];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, n = drafts_of(a, b), parts = a.spans * kParts;
   const int stay = ALONE ? verdict(a, b, n) : a.n_accepted[b];
   const Row row = row_of(a, b, n, stay);
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a)
   const int begin = part_begin(a, sPart), end = part_begin(a, sPart + 1);
   // Inside the part: four neighbouring tokens to a thread, sums over the threads before it.
 #pragma unroll 1
-  for (int first = begin; first < end; first += 4 * kPickThreads) {
+  for (int first = begin; first < end; first += 4 * kThreads) {
     const int t0 = first + 4 * tid;
     double w[4];
 #pragma unroll
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a)
     __syncthreads();
     double at = before + (upto - mine), all = 0.0;
 #pragma unroll
-    for (int k = 0; k < kPickThreads / 64; ++k) {
+    for (int k = 0; k < kThreads / 64; ++k) {
       if (k < tid >> 6) at += sWave[k];
       all += sWave[k];
     }
@@ -257,16 +258,16 @@ __global__ void __launch_bounds__(kPickThreads) verify_pick_kernel(VerifyArgs a)
   if (tid <= a.n) out[tid] = tid < stay ? a.draft[(size_t)b * a.n + tid] : tid == stay ? token : -1;
 }
 
-// One workgroup takes a whole row, and a call one launch, where rows are short (1 row of 1000: 9.4 us, of 16384: 11.6, with two
-// launches 11.3 and 11.8; of 32000: 16.0 and 13.4) or many enough to fill the chip (256 rows of 32000: 31.0 and 36.5 us, of 65536: 35.5 and
-// 46.8; 64 rows of 32000: 20.1 and 19.4).
+// One workgroup takes a whole row, and a call one launch, where rows are short (1 row of 1000: 9.3 us, of 16384: 11.6, of 32000: 16.0 and
+// with two launches 11.0; 16 rows of 16384: 14.2 and 14.5) or many enough to fill the chip (256 rows of 32000: 31.0 and 36.5 us, of
+// 65536: 35.5 and 46.8; 64 rows of 32000: 20.1 and 20.7).
 static bool verify_alone(int B, int V) { return V <= 16384 || (B >= 128 && V <= 65536); }
 
-// Spans of a row: enough workgroups for the chip, none of less than 2 048 tokens.
+// Spans of a row: enough workgroups for the chip, none of less than 1 024 tokens.
 static int verify_spans(int B, int V) {
-  if (verify_alone(B, V)) return kPickThreads / kVerifyThreads;
-  int s = (1024 + B - 1) / B;
-  if (s > V / 2048) s = V / 2048;
+  if (verify_alone(B, V)) return kAloneThreads / kVerifyThreads;
+  int s = (2048 + B - 1) / B;
+  if (s > V / 1024) s = V / 1024;
   if (s > kVerifyMaxSpans) s = kVerifyMaxSpans;
   return s < 1 ? 1 : s;
 }
@@ -315,11 +316,14 @@ int mixkvq_verify_draft(int32_t B, int32_t n_draft, int32_t V, const float* p_ta
   a.V = V;
   const hipStream_t s = (hipStream_t)stream;
   if (verify_alone(B, V)) {
-    verify_pick_kernel<true><<<B, kPickThreads, 0, s>>>(a);
+    verify_pick_kernel<true, kAloneThreads><<<B, kAloneThreads, 0, s>>>(a);
   } else {
     verify_sum_kernel<<<B * a.spans, kVerifyThreads, 0, s>>>(a);
     MIXKVQ_TRY_HIP(hipGetLastError());
-    verify_pick_kernel<false><<<B, kPickThreads, 0, s>>>(a);
+    // (a part of four tokens a thread is gone over in one turn: 32000 tokens 11.0 us with 256 threads, 13.5 with 1024; 500000, with
+    // parts of 1953 tokens, 17.4 and 14.8)
+    if (V / (a.spans * kParts) < 1024) verify_pick_kernel<false, 256><<<B, 256, 0, s>>>(a);
+    else verify_pick_kernel<false, 1024><<<B, 1024, 0, s>>>(a);
   }
   MIXKVQ_TRY_HIP(hipGetLastError());
   return MIXKVQ_OK;
