@@ -201,7 +201,7 @@ class Cache:
         h = C.c_void_p()
         _check(self.lib.mixkvq_cache_create(C.byref(cfg), C.byref(bufs), C.byref(h)))
         self.handle = h
-        self._known = (cfg.B, cfg.Hq, cfg.Hkv, cfg.D, torch.bfloat16 if cfg.in_dtype else torch.float16, self.device.index or 0)
+        self._known = (cfg.B, cfg.Hq, cfg.Hkv, cfg.D, torch.bfloat16 if cfg.in_dtype else torch.float16, self.blocks.get_device())
         self.reset()
 
     def __del__(self):
@@ -374,7 +374,7 @@ class Cache:
         if n_seq is not None:
             assert len(n_seq) == B
             counts = (C.c_int32 * B)(*n_seq)
-        with _on(self.device, stream):
+        with _on(q.device, stream):
             if out is None:
                 out = torch.empty_like(q)
             if lse is None:
