@@ -20,8 +20,8 @@
 // in turn, 8192 new tokens over an empty cache (28 query and 4 KV heads) took 645 and 581 us, and 497 us this way (967 TFLOP/s;
 // a large library product reaches 1 171 on this card).  Barriers (two to a tile), the tile's way through LDS and the start and end
 // of a workgroup take a third of the time.
-// 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 685 us, 660 TFLOP/s; 2 x 2048 after
-// 8190 (records of 32) 1119 us, 691 TFLOP/s.
+// 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 670 us, 675 TFLOP/s; 2 x 2048 after
+// 8190 (records of 32) 1105 us, 700 TFLOP/s.
 #include <type_traits>
 #include "chunk.h"
 
@@ -654,12 +654,14 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       if (next) stage(t + 1, true);
       if (next2) fetch(t + 2);
       // The wavefronts of a SIMD (w and w + 4) unpack at different times: one's vector instructions run beside the other's matrix
-      // instructions.
+      // instructions, which go first (669 and 681 us for 1000 tokens after 31000).
       if (next && wave < 4) unpack_low_keys(lds, there, map_of(t + 1), tokens_of(t + 1));
       if (REST && next) entries_next = list_entries(lds, tile_count(t + 1));
       if (active) {
+        __builtin_amdgcn_s_setprio(1);
         step<0, REST>(lds, in, t == t_first ? 0 : here - there, rest_here - here, entries, sc[0], sc[1], pw[1], pw[0], 2 * 32 > n_tok, n_tok, c, st);
         step<1, REST>(lds, in, 0, rest_here - here, entries, sc[1], sc[0], pw[0], pw[1], 3 * 32 > n_tok, n_tok, c, st);
+        __builtin_amdgcn_s_setprio(0);
       }
       if (next && wave >= 4) unpack_side_keys<REST>(lds, there, rest_there, tokens_of(t + 1));
       __syncthreads();      // the next tile's keys are there, and its values are staged
@@ -669,8 +671,10 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       }
       if (next && wave >= 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1), share, 4);
       if (active) {         // (behind the last tile: scores of what the other tile's place holds, all of them hidden)
+        __builtin_amdgcn_s_setprio(1);
         step<2, REST>(lds, in, there - here, rest_here - here, entries, sc[0], sc[1], pw[1], pw[0], 4 * 32 > n_tok, n_tok, c, st);
         step<3, REST>(lds, in, 0, rest_there - there, entries_next, sc[1], sc[0], pw[0], pw[1], 32 > n_next, n_next, c, st);
+        __builtin_amdgcn_s_setprio(0);
       }
       if (next && wave < 4) unpack_values(lds, there + kKeyBytes, tokens_of(t + 1), 0, share);
       entries = entries_next;
