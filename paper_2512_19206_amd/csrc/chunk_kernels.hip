@@ -17,7 +17,7 @@
 // exponentials; on a SIMD's two wavefronts that is 1 024 matrix and about 1 250 vector cycles, of which at best 1 320 remain
 // together (a matrix instruction holds the vector issue for 8 cycles), and 1 700 were measured.  So scores of the next slice, weights
 // of this one and values of the last one are interleaved by hand; with the compiler's order, or with products and exponentials
-// in turn, 8192 new tokens over an empty cache (28 query and 4 KV heads) took 645 and 581 us, and 497 us this way (967 TFLOP/s;
+// in turn, 8192 new tokens over an empty cache (28 query and 4 KV heads) took 645 and 581 us, and 491 us this way (980 TFLOP/s;
 // a large library product reaches 1 171 on this card).  Barriers (two to a tile), the tile's way through LDS and the start and end
 // of a workgroup take a third of the time.
 // 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 670 us, 675 TFLOP/s; 2 x 2048 after
@@ -727,8 +727,10 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       __syncthreads();      // this tile's values are there
       if (next) fetch(t + 1, true);
       if (active) {
+        __builtin_amdgcn_s_setprio(1);
         step<0, false>(lds, in, t == f_first ? 0 : here - there, 0, 0u, sc[0], sc[1], pw[1], pw[0], 2 * 32 > all, limit, c, st);
         step<1, false>(lds, in, 0, 0, 0u, sc[1], sc[0], pw[0], pw[1], 3 * 32 > all, limit, c, st);
+        __builtin_amdgcn_s_setprio(0);
       }
       if (next) {
         store(t + 1, there);
@@ -737,8 +739,10 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_attention_kernel(Chunk
       __syncthreads();      // the next tile's keys are there
       if (active) {
         const int all_next = next ? all_of(t + 1) : 0, limit_next = next ? limit_of(t + 1) : 0;
+        __builtin_amdgcn_s_setprio(1);
         step<2, false>(lds, in, there - here, 0, 0u, sc[0], sc[1], pw[1], pw[0], 4 * 32 > all, limit, c, st);
         step<3, false>(lds, in, 0, 0, 0u, sc[1], sc[0], pw[0], pw[1], 32 > all_next, limit_next, c, st);
+        __builtin_amdgcn_s_setprio(0);
       }
       if (next) store(t + 1, there + kKeyBytes);
     }
