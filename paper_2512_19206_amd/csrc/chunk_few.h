@@ -10,8 +10,12 @@
 // exactly; 4^-p goes into the scales.  q s is kept in two halves, hi = fp16(q s) and the exact remainder lo = fp16(q s - hi), so
 // a score carries about 22 bits of it: rounded to one half, 131 072 tokens with sharp weights had outputs 0.8 % off.  A packed
 // multiply and a packed multiply-add form both halves of two products.  q.z is one matrix product per group of tokens against
-// the zero-points.  With one value group to a token the same goes for the values: sum p (c s + z) = sum (p s) c + sum p z, with
-// p s rounded once; with more they are dequantized in registers (one rounding each).
+// the zero-points.
+//
+// Values are dequantized in registers, c s + z rounded once, and the sum of the weights takes them as rounded: what is left of a
+// rounding is relative to the values themselves.  (sum (p s) c + sum p z, with the scales in the weights, takes 64 vector instructions
+// less a slice; but the two sums cancel where one element of a group lies far from the others, and p s in one half was then wrong by
+// half a step of the far element: outputs 6e-3 off beside elements of 512.)
 //
 // The channels of a record stand in the order of its tiers.  Each wavefront keeps its rows of q in that order in LDS and moves
 // them only where a record's lists differ from the record's before it.  What a record begins with (lists, scales, zero-points)
@@ -35,8 +39,8 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 512, kWaves = 8;
-// log2 by which scores may pass the reference before the sums are brought to a new one: weights stay below 2^13, and with scales
-// of at most 2 inside binary16.  Most slices change nothing.
+// log2 by which scores may pass the reference before the sums are brought to a new one: weights stay below 2^13, inside binary16.
+// Most slices change nothing.
 constexpr float kHeadroom = 13.f;
 constexpr float kNoToken = -1e30f;                // reference of a row that has seen no token
 
@@ -89,7 +93,6 @@ struct Kernel {
   static constexpr int kOffScale = kOffGroup + kWaves * kGroupBytes;
   static constexpr int kLds = kOffScale + kRows * 4;
   static constexpr int kOutRow = kD + 4;                           // floats of a row where the wavefronts' results meet: sums, reference, weights
-  static constexpr bool kFold = NVG == 1;                          // value scales go into the weights, zero-points into a product of their own
   static constexpr bool kKeysEarly = NB <= 2;                      // registers for two slices' keys
   static constexpr bool kKept = NB == 1;                           // both halves of q s stay in registers through a group
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
@@ -99,8 +102,7 @@ struct Kernel {
   __device__ static __forceinline__ int piece(int r, int o) { return kPieces == 16 ? o ^ (r & 15) : kPieces == 20 ? o ^ ((r >> 1) & 3) : o ^ (r & 7); }
 
   struct State {
-    // O^T by blocks of 16 channels; the ninth is a product of the weights with ones (in row 0) and, where the value scales are
-    // folded into the weights, with the values' zero-points (in row 1): the sums of the weights and of the weighted zero-points.
+    // O^T by blocks of 16 channels; the ninth is a product of the weights with ones (in row 0): their sums.
     f4 o[NB][9];
     float m[NB];      // reference of the exponents (log2 units)
   };
@@ -133,7 +135,7 @@ struct Kernel {
 
   struct Keys { uint4 w[2]; unsigned four[2]; uint4 raw[2]; };
   struct Words { uint4 w[2]; uint4 s[NVG], z[NVG]; };
-  struct Head { int e0, e1; unsigned s[(NKC + 3) / 4], z[(NKC + 3) / 4]; unsigned short top, vtop; };
+  struct Head { int e0, e1; unsigned s[(NKC + 3) / 4], z[(NKC + 3) / 4]; unsigned short top; };
 
   template <class Counts>
   __device__ static __forceinline__ void run(const ChunkArgs& a, const Counts& counts, unsigned char* lds) {
@@ -216,13 +218,12 @@ struct Kernel {
     };
     // What a group begins with: the record's lists (entries lane and lane + 64), the group's largest scale, scales and zero-points of
     // places 2 lane and 2 lane + 1 (and 128 further).
-    const int ks = k4 + k16, gps = a.Gk >> 5, n_groups = spr / gps;      // gps: slices of a group
+    const int ks = k4 + k16, gps = a.Gk >> 5;      // gps: slices of a group
     auto load_head = [&](const uint8_t* rec, int gr, Head& h) __attribute__((always_inline)) {
       const int ln = here(lane), last = ks > 0 ? ks - 1 : 0;
       h.e0 = rec[a.off_idx + (ln < last ? ln : last)];
       h.e1 = rec[a.off_idx + (ln + 64 < last ? ln + 64 : last)];
       h.top = *reinterpret_cast<const unsigned short*>(rec + (unsigned)(a.off_kmax + 2 * gr));
-      if constexpr (kFold) h.vtop = *reinterpret_cast<const unsigned short*>(rec + (unsigned)(a.off_kmax + 2 * n_groups));
 #pragma unroll
       for (int i = 0; i < (NKC + 3) / 4; ++i) {
         const Place pl = place_of(ln, i);
@@ -299,6 +300,7 @@ struct Kernel {
 #pragma unroll
       for (int c = 0; c < 9; ++c) st.o[r][c] = f4{0.f, 0.f, 0.f, 0.f};
     }
+    const h8 ones = m16 == 0 ? splat8((_Float16)1.f) : splat8((_Float16)0.f);
     float fl[NB];
 #pragma unroll
     for (int r = 0; r < NB; ++r) fl[r] = row_scale[16 * r + m16];
@@ -363,8 +365,6 @@ struct Kernel {
       h8 hi[kKept ? NB : 1][kKept ? NKC : 1], lo[kKept ? NB : 1][kKept ? NKC : 1];
       float fg[NB], bias[NB], rho = 0.f;      // scores = codes' sums * fg + bias; fp16 tier's sums * rho join the codes'
       bool group = true;
-      int unit = 0;                    // kFold: O is kept in units of 2^-(24 + unit), scales of values enter times 2^unit
-      bool unit_set = false;
       for (int u = u0; u < end; ++u) {
         // Of two wavefronts on a SIMD the older one goes first; the younger one takes every other slice ahead of it, else it is left
         // with a part of the work that nothing overlaps.
@@ -375,20 +375,6 @@ struct Kernel {
         if (group) {
           const int gr = sl / gps;
           order_rows(lane < ks ? head.e0 : 255, lane + 64 < ks ? head.e1 : 255);
-          if constexpr (kFold) {
-            const float vtop = (float)__builtin_bit_cast(_Float16, head.vtop);
-            const int top_at = vtop > 0.f ? __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(vtop)) : -24;
-            if (!unit_set || top_at + unit > 1) {      // the largest scale becomes less than 1/2, and may grow to 2
-              const int now = -1 - top_at < 15 ? -1 - top_at : 15;      // (2^15 is a half, and lifts the smallest scale out of the subnormals)
-              const float f = ldexpf(1.f, unit_set ? now - unit : 0);
-#pragma unroll
-              for (int r = 0; r < NB; ++r)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) st.o[r][c] *= f;
-              unit = now;
-              unit_set = true;
-            }
-          }
           // the largest scale becomes 2^6 to 2^7: products with q stay below 2^14, small ones keep their bits
           const float top = (float)__builtin_bit_cast(_Float16, head.top);
           int e = top > 0.f ? 7 - __builtin_amdgcn_frexp_expf(top) : 0;
@@ -486,15 +472,6 @@ struct Kernel {
         blk = nblk;
         rec = nrec;
         group = sl % gps == 0;
-        h8 ones = splat8((_Float16)1.f);
-        h8 vf;                         // scales of the lane's tokens, with the factors of the codes: token pair x comes with 4^x
-        if constexpr (kFold) {
-          const unsigned keep = m16 == 1 ? 0xffffffffu : 0u, one = m16 == 0 ? 0x3c003c00u : 0u;
-          const uint4 z = val.z[0];
-          ones = as_h8((z.x & keep) | one, (z.y & keep) | one, (z.z & keep) | one, (z.w & keep) | one);
-          const _Float16 f = (_Float16)ldexpf(1.f, unit), q1 = (_Float16)0.25f, q2 = (_Float16)0.0625f, q3 = (_Float16)0.015625f;
-          vf = __builtin_bit_cast(h8, val.s[0]) * splat8(f) * h8{1, 1, q1, q1, q2, q2, q3, q3};
-        }
         h8 pw[NB];
 #pragma unroll
         for (int r = 0; r < NB; ++r) {
@@ -505,7 +482,6 @@ struct Kernel {
             if constexpr (HAS16) x[i] = __builtin_fmaf(s16[r][i >> 2][i & 3], rho, x[i]);
           }
           pw[r] = weigh(st, r, x, fg[r], bias[r], ones);
-          if constexpr (kFold) pw[r] *= vf;
           if constexpr (NB > 2) __builtin_amdgcn_sched_barrier(0);      // one block's scores at a time: registers
         }
         // ---- values ----
@@ -513,38 +489,23 @@ struct Kernel {
         for (int c = 0; c < 8; ++c) {
           const uint4 four_words = val.w[c >> 2];
           const unsigned x = (c & 3) == 0 ? four_words.x : (c & 3) == 1 ? four_words.y : (c & 3) == 2 ? four_words.z : four_words.w;
-          h8 v;
-          if constexpr (kFold) {
-            v = as_h8(x & mask[0], x & mask[1], x & mask[2], x & mask[3]);
-          } else {
-            unsigned sp[4], z4[4];       // pairs of tokens of the group of channel 64 (c / 4) + 4 m16 + c % 4
-            const int dw = NVG == 2 ? 0 : c >> 2;
-            const unsigned* ps = reinterpret_cast<const unsigned*>(val.s);
-            const unsigned* pz = reinterpret_cast<const unsigned*>(val.z);
-            const unsigned pick = (NVG == 2 ? c >> 2 : m16 >> 3) ? 0x07060302u : 0x05040100u;
+          unsigned sp[4], z4[4];         // pairs of tokens of the group of channel 64 (c / 4) + 4 m16 + c % 4
+          const unsigned* ps = reinterpret_cast<const unsigned*>(val.s);
+          const unsigned* pz = reinterpret_cast<const unsigned*>(val.z);
+          const int dw = NVG == 2 ? 0 : c >> 2;
+          const unsigned pick = (NVG == 2 ? c >> 2 : m16 >> 3) ? 0x07060302u : 0x05040100u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int d0 = i * NVG + dw, d1 = d0 + NVG / 2;      // of tokens 2 i and 2 i + 1
-              sp[i] = __builtin_amdgcn_perm(ps[d1], ps[d0], pick);
-              z4[i] = __builtin_amdgcn_perm(pz[d1], pz[d0], pick);
-            }
-            v = as_h8(value_pair<0>(x, mask[0], sp[0], z4[0]), value_pair<1>(x, mask[1], sp[1], z4[1]),
-                      value_pair<2>(x, mask[2], sp[2], z4[2]), value_pair<3>(x, mask[3], sp[3], z4[3]));
+          for (int i = 0; i < 4; ++i) {
+            const int d0 = NVG == 1 ? i : i * NVG + dw, d1 = d0 + NVG / 2;      // of tokens 2 i and 2 i + 1
+            sp[i] = NVG == 1 ? ps[i] : __builtin_amdgcn_perm(ps[d1], ps[d0], pick);
+            z4[i] = NVG == 1 ? pz[i] : __builtin_amdgcn_perm(pz[d1], pz[d0], pick);
           }
+          const h8 v = as_h8(value_pair<0>(x, mask[0], sp[0], z4[0]), value_pair<1>(x, mask[1], sp[1], z4[1]),
+                             value_pair<2>(x, mask[2], sp[2], z4[2]), value_pair<3>(x, mask[3], sp[3], z4[3]));
 #pragma unroll
           for (int r = 0; r < NB; ++r) st.o[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pw[r], st.o[r][c], 0, 0, 0);
         }
         load_words(rec, sl, val);
-      }
-      if constexpr (kFold) {      // O to its own units, the zero-points' part joins it
-        const float back = ldexpf(16777216.f, -unit);
-#pragma unroll
-        for (int r = 0; r < NB; ++r) {
-          const float z = __shfl(st.o[r][8][1], m16);
-#pragma unroll
-          for (int c = 0; c < 8; ++c) st.o[r][c] = st.o[r][c] * back + z;
-          st.o[r][8][1] = 0.f;
-        }
       }
     }
 
@@ -612,7 +573,7 @@ struct Kernel {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 8 * grp + e < limit ? s[r][e >> 2][e & 3] * fl[r] : -INFINITY;
-        pw[r] = weigh(st, r, x, 1.f, 0.f, m16 == 0 ? splat8((_Float16)1.f) : splat8((_Float16)0.f));
+        pw[r] = weigh(st, r, x, 1.f, 0.f, ones);
       }
       const int vrow = 8 * grp + (m16 >> 2), sub = (m16 & 1) * 8;
       typedef __attribute__((address_space(3))) s4* lds_s4;
