@@ -39,9 +39,10 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 512, kWaves = 8;
-// log2 by which scores may pass the reference before the sums are brought to a new one: weights stay below 2^13, inside binary16.
-// Most slices change nothing.
-constexpr float kHeadroom = 13.f;
+// The largest score's weight is 2^kBoost when the sums are brought to a new reference, and no weight passes 2^kHeadroom (log2), which
+// binary16 holds: most slices change nothing, and a weight counts down to 2^-33 of the largest one (with the largest one at 1 it was
+// 2^-25: a first token 2^25 ahead hid all the others, whose number makes up for that).
+constexpr float kHeadroom = 15.9f, kBoost = 8.f;
 constexpr float kNoToken = -1e30f;                // reference of a row that has seen no token
 
 __device__ __forceinline__ h2 as_h2(unsigned w) { return __builtin_bit_cast(h2, w); }
@@ -115,7 +116,7 @@ struct Kernel {
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i]);
     mx = __builtin_fmaf(mx, f, add);
     if (__any(mx > st.m[b] + kHeadroom)) {
-      const float m = fmaxf(st.m[b], max_of_groups(mx)), down = __builtin_amdgcn_exp2f(st.m[b] - m);
+      const float m = fmaxf(st.m[b], max_of_groups(mx) - kBoost), down = __builtin_amdgcn_exp2f(st.m[b] - m);
       st.m[b] = m;
 #pragma unroll
       for (int c = 0; c < 9; ++c) st.o[b][c] *= down;

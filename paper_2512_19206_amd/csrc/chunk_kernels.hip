@@ -120,9 +120,10 @@ __device__ __forceinline__ int tid_here() {
   return x;
 }
 
-// The largest score may run ahead of the reference by this much (in log2) before the sums are brought to a new reference:
-// weights stay below 2^13, well inside binary16, and most tiles change nothing.
-constexpr float kHeadroom = 13.f;
+// The largest score may run ahead of the reference by kHeadroom (in log2) before the sums are brought to a new reference, kBoost (or
+// up to one more) below it: weights stay inside binary16, most tiles change nothing, and a weight counts down to 2^-32 of the
+// largest one (with the largest one at 1 it was 2^-25: a first token 2^25 ahead hid all the others, whose number makes up for that).
+constexpr float kHeadroom = 15.9f, kBoost = 8.f;
 constexpr float kNoToken = -1e30f;      // reference of a row that has seen no token
 
 // Where a lane reads its operands: addresses that stand for a whole tile (the rest is the instructions' constant offset).  BY_CHANNEL: the
@@ -195,11 +196,11 @@ __device__ __forceinline__ float largest(const f16v& s) {
 
 // Brings the sums and the weights that are still to be used to a new reference if a score (mx: this lane's largest) has run too far
 // ahead; only then do the two lanes of a row agree on it.  References are whole numbers: the weights' factor is a power of two, taken
-// in two parts because a weight of up to 2^13 may still count when the whole factor is below binary16.
+// in two parts because a weight of nearly 2^16 may still count when the whole factor is below binary16.
 __device__ __forceinline__ void follow(float mx, Rows& st, h8 (&p)[2]) {
   if (__any(mx > st.m + kHeadroom)) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    const float m = ceilf(fmaxf(st.m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])))), back = st.m - m, f = __builtin_amdgcn_exp2f(back);
+    const float m = fmaxf(st.m, ceilf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]))) - kBoost), back = st.m - m, f = __builtin_amdgcn_exp2f(back);
     st.m = m;
     st.l *= f;
 #pragma unroll
