@@ -308,6 +308,12 @@ int mixkvq_set_timing_events(mixkvq_cache* c, void* start_event, void* stop_even
 #define MIXKVQ_PATH_VECTOR 2
 int mixkvq_decode_path(const mixkvq_cache* c);
 
+/* Profiling aid: the form of the last mixkvq_chunk_attention on this cache that launched anything, as the query rows of a workgroup.  16,
+ * 32 or 48: the kernel for few query rows, which takes records of R = 32, 64, 96, 128 or 256 with Gk a multiple of 32, at most four value
+ * groups to a token, k4 <= 32 and k16 <= 32 (48 rows: one value group, k16 = 0, and k4 = 0 or, with policy 0, 16).  256: the kernel for
+ * many, and for every other layout, where a few rows cost as much as 256.  0: no such call yet.  Host-only; negative on a NULL handle. */
+int mixkvq_chunk_path(const mixkvq_cache* c);
+
 /* Message for a return code (for EHIP: the last HIP error string seen by this thread). */
 const char* mixkvq_strerror(int code);
 

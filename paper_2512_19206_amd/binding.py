@@ -22,7 +22,7 @@ EXPORTS = ("mixkvq_block_layout", "mixkvq_cache_sizes", "mixkvq_cache_create", "
            "mixkvq_cache_set_block_table", "mixkvq_cache_set_state", "mixkvq_cache_set_state_seq", "mixkvq_cache_reset", "mixkvq_cache_reset_seq", "mixkvq_cache_state", "mixkvq_cache_state_seq",
            "mixkvq_select_channels", "mixkvq_select_channels_seq", "mixkvq_quantize_append", "mixkvq_quantize_append_seq", "mixkvq_prefill",
            "mixkvq_decode_attention", "mixkvq_decode_attention_noalloc", "mixkvq_decode_step", "mixkvq_set_timing_events", "mixkvq_decode_path",
-           "mixkvq_chunk_workspace", "mixkvq_chunk_attention", "mixkvq_verify_workspace", "mixkvq_verify_draft",
+           "mixkvq_chunk_workspace", "mixkvq_chunk_attention", "mixkvq_chunk_path", "mixkvq_verify_workspace", "mixkvq_verify_draft",
            "mixkvq_strerror")
 
 
@@ -91,6 +91,7 @@ def load_library() -> C.CDLL:
     i64, i32p = C.c_int64, C.POINTER(C.c_int32)
     lib.mixkvq_chunk_workspace.argtypes = [vp, i32, i32p]
     lib.mixkvq_chunk_attention.argtypes = [vp, vp, i64p, vp, vp, i64p, i32, i32p, vp, i64p, vp, C.c_float, i32, vp, i64, vp]
+    lib.mixkvq_chunk_path.argtypes = [vp]
     lib.mixkvq_verify_workspace.argtypes = [i32, i32]
     lib.mixkvq_verify_draft.argtypes = [i32, i32, i32, vp, i64p, vp, i64p, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.mixkvq_strerror.argtypes = [i32]
@@ -401,6 +402,10 @@ class Cache:
     def decode_path(self) -> int:
         """Kernel of the last attention call: PATH_NONE, PATH_MATRIX (matrix-core kernel) or PATH_VECTOR (fallback)."""
         return int(self.lib.mixkvq_decode_path(self.handle))
+
+    def chunk_path(self) -> int:
+        """Query rows of a workgroup in the last chunk_attention call: 16, 32 or 48 (the kernel for few rows), 256 (for many) or 0."""
+        return int(self.lib.mixkvq_chunk_path(self.handle))
 
     # helpers for tests: views of the raw buffers
     def block_records(self) -> torch.Tensor:

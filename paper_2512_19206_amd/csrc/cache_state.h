@@ -15,6 +15,7 @@ struct mixkvq_cache {
   SeqState* seq;         // [B]: every sequence has its own counts (they are equal while the batch runs in lock-step)
   hipEvent_t ev_start = nullptr, ev_stop = nullptr;   // optional timing of the split kernel
   int last_path = MIXKVQ_PATH_NONE;                   // kernel of the last attention launch
+  int last_chunk = 0;                                 // query rows of a workgroup in the last launch of several new tokens
   bool tickets_clear = false;                         // the ticket words were set to 0 once
 };
 

@@ -278,10 +278,13 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
     if (l.units == 0) continue;
     ChunkCounts counts;
     fill_launch(c, pl, l, n_new, n_seq, &a, &counts);
+    c->last_chunk = pl.rows;
     MIXKVQ_TRY_HIP(launch_chunk(a, l.equal ? nullptr : &counts, l.units, l.n, pl.few, pl.rows, s));
     if (accumulate_q) MIXKVQ_TRY_HIP(launch_chunk_books(v, a, l.equal ? nullptr : &counts, l.n, l.most, s));
   }
   return MIXKVQ_OK;
 }
+
+int mixkvq_chunk_path(const mixkvq_cache* c) { return c ? c->last_chunk : MIXKVQ_EINVAL; }
 
 }  // extern "C"
