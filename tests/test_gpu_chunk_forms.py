@@ -1,5 +1,6 @@
 """Every form of mixkvq_chunk_attention's kernels: blocks of query rows, steps of channel places, the fp16 tier, value groups, with and
-without splits, equal and ragged batches.  Each test says which form it is about and holds the call to it."""
+without splits, equal and ragged batches; and what their running references and records of very different scales have to carry through
+several packed records of one wavefront.  Each test says which form it is about and holds the call to it."""
 import numpy as np
 import pytest
 import torch
@@ -124,3 +125,61 @@ def test_layouts_that_only_the_kernel_for_many_rows_takes(H, layout):
     out, lse = M.mixkvq_chunk_attention(gc, q, k, v)
     assert gc.chunk_path() == 256
     _check(deq, g, q, k, v, out, lse, [n] * B, [(0, 0), (0, 1), (1, 0), (1, 1)], 1 / np.sqrt(128.0), True, 2.0 ** -30)
+
+
+# Few rows: 14, 21 and 35 of a KV head in batches that leave every wavefront several slices; many: 560.
+FORMS = [(64, 4, 7, 2, 16), (64, 4, 7, 3, 32), (64, 4, 7, 5, 48), (1, 1, 7, 80, 256)]
+
+
+@pytest.mark.parametrize("B,Hkv,g,n,rows", FORMS, ids=lambda x: str(x))
+@pytest.mark.parametrize("R,Gk,Gv,k4,k16", [(128, 128, 128, 16, 0), (32, 32, 128, 0, 4), (128, 32, 32, 8, 4), (32, 32, 64, 16, 0)])
+@pytest.mark.parametrize("jump", [20.0, 25.0, 60.0])
+def test_scores_that_jump_inside_packed_records(H, B, Hkv, g, n, rows, R, Gk, Gv, k4, k16, jump):
+    """Scores (in powers of two) of 0, then of 12.9 on 24 tokens, then one of `jump` and one of twice that, over and over through 1900
+    packed tokens: every wavefront meets them in its own run, and what 24 weights carry must not be lost where the sums change their
+    reference."""
+    import paper_2512_19206_amd as M
+    if rows == 48 and not _forty_eight(k4, k16, Gv):
+        rows = 32
+    rng = np.random.default_rng(54)
+    T = 1900
+    K, V = np.zeros((1, T, 128), np.float16), rng.standard_normal((1, T, 128)).astype(np.float16)
+    for t in range(0, T - 200, 190):
+        K[0, t + 40:t + 64, 0], V[0, t + 40:t + 64] = 12.9, 8.0
+        K[0, t + 100, 0], K[0, t + 165, 0] = jump, 2 * jump
+    gc, deq = _batch(H, B, Hkv, g, K, V, [T], T_max=1920, R=R, Gk=Gk, Gv=Gv, k4=k4, k16=k16)
+    q = torch.zeros(B, Hkv * g, n, 128, dtype=torch.float16, device="cuda")
+    q[..., 0] = float(np.log(2.0))
+    v = _new(rng, B, Hkv, n)
+    k = torch.zeros_like(v)
+    out, lse = M.mixkvq_chunk_attention(gc, q, k, v, scale=1.0)
+    assert gc.chunk_path() == rows
+    _check(deq, g, q, k, v, out, lse, [n] * B, [(0, 0), (B - 1, Hkv - 1)], 1.0, rows == 256, 2.0 ** -30)
+
+
+@pytest.mark.parametrize("B,Hkv,g,n,rows", FORMS, ids=lambda x: str(x))
+@pytest.mark.parametrize("R,Gk,Gv", [(128, 128, 128), (32, 32, 128), (32, 32, 32)])
+@pytest.mark.parametrize("lead", [False, True])
+def test_records_of_very_different_scales(H, B, Hkv, g, n, rows, R, Gk, Gv, lead):
+    """Values (and keys) whose scales change by 2^6 to 2^12 from one record to the next, up and down; with lead, a token of the first
+    record has the largest score by far, so that everything else counts little."""
+    import paper_2512_19206_amd as M
+    if rows == 48 and Gv != 128:
+        rows = 32
+    rng = np.random.default_rng(55)
+    T, B_ = 1900, B
+    size = np.array([1.0, 64.0, 2.0 ** -6, 2048.0, 1.0, 2.0 ** -6, 4096.0, 0.25])[np.arange(T) // R % 8][None, :, None]
+    V = (rng.standard_normal((1, T, 128)) * size).astype(np.float16)
+    K = (rng.standard_normal((1, T, 128)) * np.minimum(size, 8.0) * 0.3).astype(np.float16)
+    K[0, 5, :] = 0.0
+    if lead:
+        K[..., 0], V[0, 5] = 0.0, 0.0
+        K[0, 5, 0] = 16.0
+    gc, deq = _batch(H, B_, Hkv, g, K, V, [T], T_max=1920, R=R, Gk=Gk, Gv=Gv, k4=16, k16=0)
+    q, k, v = _new(rng, B, Hkv * g, n, 0.5), _new(rng, B, Hkv, n, 0.5), _new(rng, B, Hkv, n)
+    if lead:
+        q[..., 0] = 8.0      # the leading score: 16 * 8 / 11.3 = 11.3, 2^16
+        k[..., 0] = 0.0
+    out, lse = M.mixkvq_chunk_attention(gc, q, k, v)
+    assert gc.chunk_path() == rows
+    _check(deq, g, q, k, v, out, lse, [n] * B, [(0, 0), (B - 1, Hkv - 1)], 1 / np.sqrt(128.0), rows == 256, 2.0 ** -30)
