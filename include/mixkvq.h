@@ -249,8 +249,9 @@ int mixkvq_decode_step(mixkvq_cache* c, const void* k_new, const void* v_new, co
  *   n_seq  HOST int32 [B] or NULL: new tokens of each sequence, 0 .. n_new (NULL: n_new for all).  Rows of q, k_new and v_new
  *        behind them are not read, rows of out and lse behind them are left as they are.
  *   out  DEVICE fp16 [B][Hq][n_new][D], strides out_strides;  lse DEVICE fp32 [B][Hq][n_new] contiguous, or NULL.
- *   Channel stride 1; q, k_new, v_new and out start on 16 bytes and their strides are multiples of 8.  n_new <= 2^20, and the
- *   tiles of 16 query rows of all (sequence, KV head) pairs, at n_new tokens each, are fewer than 2^25.
+ *   Channel stride 1; q, k_new, v_new and out start on 16 bytes and their strides are multiples of 8 (that of a dimension of one
+ *   element is of no account).  n_new <= 2^20, and the tiles of 16 query rows of all (sequence, KV head) pairs, at n_new tokens each,
+ *   are fewer than 2^25.
  *   scale <= 0 means 1/sqrt(D).  accumulate_q != 0 also adds |q| of all the new tokens to the accumulator (Appendix D.2).
  *   workspace  DEVICE, on 16 bytes, at least mixkvq_chunk_workspace(c, n_new, n_seq) bytes for the cache's state at the call (NULL if
  *        that is 0), else ESCRATCH.  It needs no clearing and holds nothing between calls; calls that may overlap

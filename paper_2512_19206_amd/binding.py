@@ -369,7 +369,9 @@ class Cache:
         B, Hq, n, D = shape = q.shape
         B_, Hq_, Hkv, D_, dt, at = self._known
         assert B == B_ and Hq == Hq_ and D == D_ and k_new.shape == (B, Hkv, n, D) == v_new.shape
-        assert k_new.stride() == v_new.stride() and q.dtype == k_new.dtype == v_new.dtype == dt
+        ks, vs = k_new.stride(), v_new.stride()
+        assert ks == vs or all(size == 1 or x == y for size, x, y in zip(k_new.shape, ks, vs))
+        assert q.dtype == k_new.dtype == v_new.dtype == dt
         assert q.get_device() == k_new.get_device() == v_new.get_device() == at
         counts = None
         if n_seq is not None:

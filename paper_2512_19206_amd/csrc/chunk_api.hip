@@ -176,11 +176,9 @@ static int check_counts(const mixkvq_cache* c, int n_max, const int32_t* n_seq) 
   return MIXKVQ_OK;
 }
 
-static bool rows_ok(const void* p, const int64_t* strides) {      // rows are moved with 16-byte accesses
+static bool rows_ok(const void* p, const int64_t* strides, int B, int heads, int n) {      // rows are moved with 16-byte accesses
   if (!p || ((uintptr_t)p & 15u) || !strides) return false;
-  for (int i = 0; i < 3; ++i)
-    if (strides[i] % 8 != 0) return false;
-  return true;
+  return (B == 1 || strides[0] % 8 == 0) && (heads == 1 || strides[1] % 8 == 0) && (n == 1 || strides[2] % 8 == 0);
 }
 
 }  // namespace mixkvq
@@ -208,11 +206,12 @@ int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strid
   int rc = check_counts(c, n_new, n_seq);
   if (rc != MIXKVQ_OK) return rc;
   if (n_new == 0) return MIXKVQ_OK;
-  if (!rows_ok(q, q_strides) || !rows_ok(k_new, kv_strides) || !rows_ok(v_new, kv_strides) || !rows_ok(out, out_strides)) return MIXKVQ_EINVAL;
+  const mixkvq_config& cfg = c->v.cfg;
+  if (!rows_ok(q, q_strides, cfg.B, cfg.Hq, n_new) || !rows_ok(out, out_strides, cfg.B, cfg.Hq, n_new)) return MIXKVQ_EINVAL;
+  if (!rows_ok(k_new, kv_strides, cfg.B, cfg.Hkv, n_new) || !rows_ok(v_new, kv_strides, cfg.B, cfg.Hkv, n_new)) return MIXKVQ_EINVAL;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)kD);
   if (!(scale < INFINITY)) return MIXKVQ_EINVAL;
-  if (kv_strides[2] != (int32_t)kv_strides[2]) return MIXKVQ_EINVAL;      // (row numbers times it are formed by a 32-bit multiply)
-  const mixkvq_config& cfg = c->v.cfg;
+  if (n_new > 1 && kv_strides[2] != (int32_t)kv_strides[2]) return MIXKVQ_EINVAL;      // (row numbers times it are formed by a 32-bit multiply)
   if ((workspace && ((uintptr_t)workspace & 15u)) || workspace_bytes < 0) return MIXKVQ_EINVAL;
   const ChunkPlan pl = plan_chunk(c, n_new, n_seq);
   ChunkArgs a{};
