@@ -252,7 +252,10 @@ int mixkvq_decode_step(mixkvq_cache* c, const void* k_new, const void* v_new, co
  *   Channel stride 1; q, k_new, v_new and out start on 16 bytes and their strides are multiples of 8 (that of a dimension of one
  *   element is of no account).  n_new <= 2^20, and the tiles of 16 query rows of all (sequence, KV head) pairs, at n_new tokens each,
  *   are fewer than 2^25.
- *   scale <= 0 means 1/sqrt(D).  accumulate_q != 0 also adds |q| of all the new tokens to the accumulator (Appendix D.2).
+ *   scale <= 0 means 1/sqrt(D).  accumulate_q != 0 also adds |q| of all the new tokens to the accumulator (Appendix D.2): right for a
+ *        piece of a prompt whose queries no other call counts (mixkvq_prefill and mixkvq_select_channels do).  Of drafted tokens only
+ *        those that stay belong there: leave it 0, and behind the verdict add theirs by mixkvq_select_channels_seq (its selection may
+ *        be dropped), ahead of mixkvq_quantize_append_seq.
  *   workspace  DEVICE, on 16 bytes, at least mixkvq_chunk_workspace(c, n_new, n_seq) bytes for the cache's state at the call (NULL if
  *        that is 0), else ESCRATCH.  It needs no clearing and holds nothing between calls; calls that may overlap
  *        (two streams, two captured graphs) need one each.
