@@ -263,11 +263,13 @@ int mixkvq_decode_step(mixkvq_cache* c, const void* k_new, const void* v_new, co
  * n_seq's, are those of the call: a captured call replays with the counts of its capture.  out and lse overlap none of
  * the inputs.  Values that are not finite are outside the contract, in tokens that a row does not see as well.
  * Precision: sums are binary32, the weights of the softmax and dequantized values are rounded to binary16 (saturating) before
- * their product.  With few query rows per KV head the keys enter without a rounding of their own (the queries times their scales,
+ * their product; a weight counts down to 2^-30 of its row's largest one, and the sum (and with it lse, by up to 2^-11) is that of the
+ * weights as rounded.  With few query rows per KV head the keys enter without a rounding of their own (the queries times their scales,
  * to 22 bits, against the codes); with many each dequantized key is rounded to binary16, except that a 4-bit tier of up to 16
- * channels in blocks of a multiple of 32 tokens keeps what that drops.  A score is then off by up to 2^-11 of the sum of |q k|
- * over the other channels, which the bound of mixkvq_decode_attention covers for scores of ordinary size but not for sharp
- * softmaxes over scores in the tens.  Which of the two forms a call takes depends on its sizes alone. */
+ * channels in blocks of a multiple of 32 tokens keeps what that drops (where 128 tokens' records take up to 16 KB).  A score is then
+ * off by up to 2^-11 of the sum of |q k| over the other channels, which the bound of mixkvq_decode_attention covers for scores of
+ * ordinary size but not for sharp softmaxes over scores in the tens.  Which of the two forms a call takes depends on its sizes alone
+ * (mixkvq_chunk_path tells). */
 int64_t mixkvq_chunk_workspace(const mixkvq_cache* c, int32_t n_new, const int32_t* n_seq);   /* bytes, or a negative code */
 int mixkvq_chunk_attention(mixkvq_cache* c, const void* q, const int64_t q_strides[3], const void* k_new, const void* v_new,
                            const int64_t kv_strides[3], int32_t n_new, const int32_t* n_seq, void* out,

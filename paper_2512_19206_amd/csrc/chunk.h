@@ -82,7 +82,7 @@ __device__ __forceinline__ ChunkPlace chunk_place(const ChunkArgs& a, const Chun
   return w;
 }
 
-// rows: query rows of a workgroup (tile kernel 128 or 256; few rows 16, 32 or 48).  c == nullptr: equal counts.
+// rows: query rows of a workgroup (256, or with few rows 16, 32 or 48).  c == nullptr: equal counts.
 hipError_t launch_chunk(const ChunkArgs& a, const ChunkCounts* c, int units, int n_seq, bool few, int rows, hipStream_t s);
 hipError_t launch_chunk_books(const CacheView& v, const ChunkArgs& a, const ChunkCounts* c, int n_seq, int n_most, hipStream_t s);      // |q| of the chunk
 int chunk_tile_records(const CacheView& v);      // records of one tile

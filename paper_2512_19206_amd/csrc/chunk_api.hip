@@ -35,9 +35,10 @@ static int splits_of(int steps, int chain) {
 // The cut of a call for one kernel and tile of rows that takes the least time, and that time in microseconds.  A unit (one split of
 // one tile of rows) costs its steps and a constant part.  Workgroups of one length run in rounds; of several (later rows of a
 // chunk see more tokens, and the longest start first) they fill the compute units evenly until the shortest ones end.  Splits have
-// to be merged, which costs a launch and their rows' traffic.  The constants fit what was measured for cuts of 1 to 258 steps, e.g.
-// 48 rows (8 sequences of 32k): 17 steps a unit 66 us, 9 steps 83, 19 steps 69; 16 rows (one of 32k): 9 steps 28 us, 5 steps 39;
-// tiles (1000 after 31000 tokens): 28 steps 653 us, 14 steps 742, 126 steps 678; (8192 tokens, empty cache): unsplit 508 us, 32 steps 595.
+// to be merged, which costs a launch and their rows' traffic.  The constants fit what was measured for cuts of 1 to 258 steps, by about a
+// tenth; now, a pass (28 query and 4 KV heads): 48 rows (8 sequences of 32805): 17 steps a unit 62 us, 9 steps 80, 19 steps 68; 16 rows
+// (one of 32805): 5 steps 25 us, 9 steps 26, 17 steps 33; tiles (1000 after 31000 tokens): 28 steps 684 us, 14 steps 760, 126 steps 692;
+// (8192 tokens, empty cache): unsplit 500 us, 32 steps 575.
 static double cut_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq, ChunkPlan* pl) {
   static const int kTry[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 14, 16, 20, 24, 28, 32, 40, 48, 56, 64};
   constexpr int kTries = sizeof kTry / sizeof kTry[0];
@@ -90,10 +91,10 @@ static double cut_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq, 
 }
 
 // The kernel for few rows reads every record anew for each 16, 32 or 48 of them, the one with tiles of 256 rows dequantizes it once in
-// LDS.  Tiles of 16 rows are the quickest ones where they leave compute units idle (35 rows: a window of 90 tokens 7.0, 9.4 and 11.1 us,
-// 3000 tokens 16.7, 19.8 and 22.9, 32805 tokens 27.6, 32.5 and 38.7), of 48 where they do not (8 sequences of 32805: 82, 77 and 66 us).
-// Where the tiles of 256 start to win depends on that as well: 24 sequences of 8k tokens, 161 rows, 297 and 195 us; 8 of 16k, 161
-// rows, 106 and 118 us, 196 rows, 148 and 121 us; one of 32k, 259 rows, 58 and 78 us.
+// LDS.  Tiles of 16 rows are the quickest ones where they leave compute units idle (35 rows: a window of 90 tokens 6.7, 8.7 and 10.9 us,
+// 3000 tokens 16.1, 19.1 and 22.2, 32805 tokens 27.5, 31.8 and 37.5), of 48 where they do not (8 sequences of 32805: 85, 75 and 62 us).
+// Where the tiles of 256 start to win depends on that as well: 24 sequences of 8192 tokens, 161 rows, 185 (48 rows) and 179 us; 8 of 16384,
+// 161 rows, 99 and 114 us, 196 rows, 127 (32 rows) and 116 us; one of 32768, 259 rows, 54 and 80 us.
 static ChunkPlan plan_chunk(const mixkvq_cache* c, int n_max, const int32_t* n_seq) {
   int most = 0;
   for (int b = 0; b < c->v.cfg.B; ++b) most = n_new_of(n_seq, n_max, b) > most ? n_new_of(n_seq, n_max, b) : most;

@@ -14,17 +14,18 @@
 //
 // Values are dequantized in registers, c s + z rounded once, and the sum of the weights takes them as rounded: what is left of a
 // rounding is relative to the values themselves.  (sum (p s) c + sum p z, with the scales in the weights, takes 64 vector instructions
-// less a slice; but the two sums cancel where one element of a group lies far from the others, and p s in one half was then wrong by
-// half a step of the far element: outputs 6e-3 off beside elements of 512.)
+// less a slice, 2 to 6 % of the time; but the two sums cancel where one element of a group lies far from the others, and p s in one half
+// was then wrong by half a step of the far element: outputs up to 4e-2 off beside elements of 512.)
 //
 // The channels of a record stand in the order of its tiers.  Each wavefront keeps its rows of q in that order in LDS and moves
 // them only where a record's lists differ from the record's before it.  What a record begins with (lists, scales, zero-points)
 // is asked for a record ahead, and the scales wait in LDS, not in registers.
 //
 // What bounds it: vector issue.  64 sequences of 32790 tokens with 4 new ones each (40 query and 8 KV heads, K 2-bit with 12 channels
-// fp16, V 2-bit) take 532 us, 3.1 TB/s, with the vector ALU issuing 67 % and the matrix cores busy 38 % of the time; 4 of 131091
-// with 9 new ones 170 us.  Short runs are bound by what stands around them: of the 60 us of 8 sequences of 32805 tokens a start of 2 us, the
-// queries' first order 4 us, the last uneven slices and the meeting of the wavefronts 6 us, the launch that merges splits 7 us.
+// fp16, V 2-bit) take 567 us a pass, 2.9 TB/s, with the vector ALU issuing 68 % and the matrix cores busy 37 % of the time; 4 of 131091
+// with 9 new ones 183 us.  Short runs are bound by what stands around them: of the 62 us of 8 sequences of 32805 tokens with 5 new ones a
+// start of 2 us, the queries' first order 4 us, the last uneven slices and the meeting of the wavefronts 6 us, the launch that merges
+// splits 6 us.
 #pragma once
 #include "chunk.h"
 

@@ -17,11 +17,11 @@
 // exponentials; on a SIMD's two wavefronts that is 1 024 matrix and about 1 250 vector cycles, of which at best 1 320 remain
 // together (a matrix instruction holds the vector issue for 8 cycles), and 1 700 were measured.  So scores of the next slice, weights
 // of this one and values of the last one are interleaved by hand; with the compiler's order, or with products and exponentials
-// in turn, 8192 new tokens over an empty cache (28 query and 4 KV heads) took 645 and 581 us, and 491 us this way (980 TFLOP/s;
+// in turn, 8192 new tokens over an empty cache (28 query and 4 KV heads) took 645 and 581 us, and 500 us a pass this way (960 TFLOP/s;
 // a large library product reaches 1 171 on this card).  Barriers (two to a tile), the tile's way through LDS and the start and end
 // of a workgroup take a third of the time.
-// 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 670 us, 675 TFLOP/s; 2 x 2048 after
-// 8190 (records of 32) 1105 us, 700 TFLOP/s.
+// 1000 new tokens after 31000 cached ones (K 2-bit with 16 channels 4-bit, V 2-bit, bfloat16) take 682 us a pass, 662 TFLOP/s; 2 x 2048
+// after 8190 (records of 32) 1105 us, 700 TFLOP/s.
 #include <type_traits>
 #include "chunk.h"
 
