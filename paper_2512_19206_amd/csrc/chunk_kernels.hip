@@ -800,10 +800,14 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a, Counts co
   int pair = blockIdx.x / per_pair;
   const int i = pair / a.Hkv, j = pair % a.Hkv;
   ChunkPlace at;
-  if constexpr (std::is_same<Counts, NoChunkCounts>::value) at = chunk_place(a, counts, i * a.n_splits * a.Hkv + j);
-  else at = chunk_place(a, counts, counts.first[i] * a.Hkv + j);
+  if constexpr (std::is_same<Counts, NoChunkCounts>::value) {
+    at = chunk_place(a, counts, i * a.n_splits * a.Hkv + j);
+  } else {
+    if (counts.n_new[i] == 0) return;      // (no unit is its own; the one behind the launch's last has no place in the list)
+    at = chunk_place(a, counts, counts.first[i] * a.Hkv + j);
+  }
   const int g = a.g, n_rows = at.n_new * g, rr = blockIdx.x % per_pair * 16 + (threadIdx.x >> 4), chan = (threadIdx.x & 15) * 8;
-  if (rr >= n_rows || at.b != a.b0 + i) return;      // (a sequence without new tokens has no unit)
+  if (rr >= n_rows) return;
   const size_t first = ((size_t)at.first_block * a.row_tiles + rr / rows) * rows + rr % rows, step = (size_t)a.Hkv * a.row_tiles * rows;
   const float2* ml = reinterpret_cast<const float2*>(a.part + (size_t)blocks * rows * kD);
   float m = kNoToken, sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
