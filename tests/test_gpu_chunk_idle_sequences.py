@@ -12,7 +12,7 @@ def test_idle_sequences_in_a_split_batch(n):
     import paper_2512_19206_amd as M
     rng = np.random.default_rng(81)
     B, Hkv, g, T = 9, 2, 6, 3000
-    gc = M.Cache(M.make_config(B=B, Hq=Hkv * g, Hkv=Hkv, D=128, T_max=3072, Gk=128, Gv=128, R=128, k4=16, k16=0))
+    gc = M.Cache(M.make_config(B=B, Hq=Hkv * g, Hkv=Hkv, D=128, T_max=3200, Gk=128, Gv=128, R=128, k4=16, k16=0))
     half = lambda *shape: torch.from_numpy(rng.standard_normal(shape).astype(np.float16)).cuda()
     for b in range(B):
         m = T - 317 * b
